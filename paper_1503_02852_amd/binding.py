@@ -19,9 +19,30 @@ EXPORTS = ["rnn_graph_create", "rnn_graph_destroy", "rnn_graph_schedule", "rnn_p
            "rnn_forward_static", "rnn_last_error"]
 # measurement and inspection aids (include/rnngraph_aux.h)
 AUX_EXPORTS = ["rnn_step_build", "rnn_debug_read_control", "rnn_profile_enable", "rnn_profile_read", "rnn_plan_work"]
+# layers on the caller's own tensors (include/rnngraph_layers.h)
+LAYER_EXPORTS = ["rnn_linear_attention_workspace_bytes", "rnn_linear_attention_forward", "rnn_linear_attention_backward",
+                 "rnn_add_norm_forward", "rnn_add_norm_e4m3", "rnn_add_norm_workspace_bytes", "rnn_add_norm_backward", "rnn_dropout"]
 BUILD_NAMES = {0: "none", 1: "wave", 2: "matrix", 3: "matrix_2d", 4: "lds", 5: "interpreted", 6: "per_frame", 7: "streaming"}
 
 _lib = None
+
+
+class LinearAttentionDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "N", "heads", "kv_heads", "dim_k", "dim_v", "dtype")] + [("scale", C.c_float)]
+
+
+class Frames(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_t", C.c_int64), ("stride_n", C.c_int64), ("stride_h", C.c_int64)]
+
+
+class AddNormDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float), ("dropout", C.c_float),
+                ("seed", C.c_uint64), ("offset", C.c_uint64), ("d_offset", C.c_void_p)]
+
+
+class DropoutDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int32), ("dtype", C.c_int32), ("p", C.c_float),
+                ("seed", C.c_uint64), ("offset", C.c_uint64), ("d_offset", C.c_void_p)]
 
 
 class RnnError(RuntimeError):
@@ -90,6 +111,24 @@ def load_library(build_if_missing=True):
     lib.rnn_profile_enable.restype = C.c_int
     lib.rnn_profile_read.argtypes = [vp, C.c_int32, C.POINTER(C.c_double), i64p]
     lib.rnn_profile_read.restype = C.c_int
+    i64, fp = C.c_int64, C.POINTER(Frames)
+    attention, norm = C.POINTER(LinearAttentionDesc), C.POINTER(AddNormDesc)
+    lib.rnn_linear_attention_workspace_bytes.argtypes = [attention, C.c_int32]
+    lib.rnn_linear_attention_workspace_bytes.restype = i64
+    lib.rnn_linear_attention_forward.argtypes = [attention, fp, fp, fp, vp, vp, vp, vp, fp, vp, i64, vp]
+    lib.rnn_linear_attention_forward.restype = C.c_int
+    lib.rnn_linear_attention_backward.argtypes = [attention, fp, fp, fp, vp, vp, vp, fp, vp, fp, fp, fp, vp, vp, i64, vp]
+    lib.rnn_linear_attention_backward.restype = C.c_int
+    lib.rnn_add_norm_forward.argtypes = [norm, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp]
+    lib.rnn_add_norm_forward.restype = C.c_int
+    lib.rnn_add_norm_e4m3.argtypes = [norm, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, C.c_int32, vp, vp]
+    lib.rnn_add_norm_e4m3.restype = C.c_int
+    lib.rnn_add_norm_workspace_bytes.argtypes = [norm]
+    lib.rnn_add_norm_workspace_bytes.restype = i64
+    lib.rnn_add_norm_backward.argtypes = [norm, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, vp, i64, vp]
+    lib.rnn_add_norm_backward.restype = C.c_int
+    lib.rnn_dropout.argtypes = [C.POINTER(DropoutDesc), vp, i64, vp, i64, vp]
+    lib.rnn_dropout.restype = C.c_int
     lib.rnn_last_error.argtypes = []
     lib.rnn_last_error.restype = C.c_char_p
     _lib = lib

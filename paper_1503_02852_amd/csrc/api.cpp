@@ -17,6 +17,7 @@
 #include "../../include/rnngraph_aux.h"
 #include "jit.h"
 #include "kernels.h"
+#include "layers.h"
 #include "plan.h"
 
 using namespace rnng;
@@ -101,6 +102,9 @@ Layout make_layout(const Plan& P, int T, int N, int64_t partial_floats, bool tra
 }
 
 }  // namespace
+
+int rnng::set_error(int code, const std::string& msg) { return fail(code, msg); }
+int rnng::set_hip_error(hipError_t e, const char* what) { return fail_hip(e, what); }
 
 // Optional kernel-class timing with HIP events on the caller's stream.
 struct Profiler {

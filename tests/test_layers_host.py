@@ -1,0 +1,131 @@
+"""Host side of include/rnngraph_layers.h: symbols, workspace sizes, refusals.  Nothing here reaches a launch."""
+import ctypes as C
+import os
+import re
+
+import pytest
+
+from paper_1503_02852_amd import LAYER_EXPORTS, load_library
+from paper_1503_02852_amd.binding import AddNormDesc, DropoutDesc, Frames, LinearAttentionDesc
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 1 << 20      # an address that nothing reads
+INVALID, WORKSPACE = -1, -3
+
+
+def attention(**kw):
+    d = dict(T=8, N=2, heads=4, kv_heads=2, dim_k=16, dim_v=24, dtype=1, scale=0.25)
+    d.update(kw)
+    return C.byref(LinearAttentionDesc(*d.values()))
+
+
+def frames(p=P):
+    return C.byref(Frames(p, 64, 32, 16))
+
+
+def norm(**kw):
+    d = dict(rows=3, dim=40, dtype=1, eps=1e-6, dropout=0.0, seed=1, offset=0, d_offset=None)
+    d.update(kw)
+    return C.byref(AddNormDesc(*d.values()))
+
+
+def drop(**kw):
+    d = dict(rows=3, dim=40, dtype=1, p=0.5, seed=1, offset=0, d_offset=None)
+    d.update(kw)
+    return C.byref(DropoutDesc(*d.values()))
+
+
+def refused(rc, word, code=INVALID):
+    assert rc == code, rc
+    assert word in load_library().rnn_last_error().decode(), load_library().rnn_last_error()
+
+
+def test_library_exports_every_declared_symbol():
+    header = open(os.path.join(ROOT, "include", "rnngraph_layers.h")).read()
+    declared = set(re.findall(r"^(?:int|int64_t)\s+(rnn_[a-z0-9_]+)\s*\(", header, flags=re.M))
+    assert declared == set(LAYER_EXPORTS)
+    assert all(hasattr(load_library(), n) for n in declared)
+
+
+@pytest.mark.parametrize("bad,word", [
+    (dict(T=-1), "T and N"), (dict(N=-2), "T and N"), (dict(T=1 << 20, N=1 << 11), "2^31"), (dict(heads=0), "multiple"), (dict(kv_heads=0), "multiple"),
+    (dict(heads=3), "multiple"), (dict(N=1 << 19), "2^20"), (dict(dim_k=0), "dim_k"), (dict(dim_k=257), "dim_k"), (dict(dim_v=257), "dim_v"),
+    (dict(dtype=2), "dtype"), (dict(dtype=-1), "dtype"), (dict(scale=float("nan")), "scale"), (dict(scale=float("inf")), "scale")])
+def test_attention_descriptor_refusals(bad, word):
+    lib = load_library()
+    refused(lib.rnn_linear_attention_workspace_bytes(attention(**bad), 0), word)
+    refused(lib.rnn_linear_attention_forward(attention(**bad), frames(), frames(), frames(), P, None, None, None, frames(), None, 0, None), word)
+    refused(lib.rnn_linear_attention_backward(attention(**bad), frames(), frames(), frames(), P, None, None, frames(), None, frames(), None, None, None, None, 0, None), word)
+
+
+def test_attention_argument_refusals():
+    lib = load_library()
+    fwd = lambda q=frames(), k=frames(), v=frames(), a=P, s_in=None, s_out=None, o=frames(), d=attention(): \
+        lib.rnn_linear_attention_forward(d, q, k, v, a, None, s_in, s_out, o, None, 0, None)  # noqa: E731
+    refused(lib.rnn_linear_attention_workspace_bytes(None, 0), "descriptor")
+    refused(fwd(d=None), "descriptor")
+    for none in (None, frames(None)):
+        refused(fwd(q=none), "q pointer")
+        refused(fwd(k=none), "k pointer")
+        refused(fwd(v=none), "v pointer")
+        refused(fwd(o=none), "neither")
+    refused(fwd(a=None), "log_decay")
+    refused(fwd(q=frames(P + 1)), "aligned")
+    refused(fwd(d=attention(dtype=0), o=frames(P + 2)), "aligned")
+    refused(fwd(s_in=P + 2), "state_in")
+    refused(fwd(s_out=P + 2), "state_out")
+    assert fwd(d=attention(N=0), q=None, k=None, v=None) == 0      # nothing to do
+    back = lambda do=frames(), dq=frames(), dk=frames(), dv=frames(), ds_out=None, ds=None, ws=P, size=1 << 30, d=attention(): \
+        lib.rnn_linear_attention_backward(d, frames(), frames(), frames(), P, None, None, do, ds_out, dq, dk, dv, ds, ws, size, None)  # noqa: E731
+    refused(back(do=None), "do pointer")
+    refused(back(dk=frames(P + 1)), "dk")
+    refused(back(ds_out=P, ds=P), "dstate")
+    need = lib.rnn_linear_attention_workspace_bytes(attention(), 1)
+    assert need >= 8 * 2 * 4 * (16 + 24) * 4      # the heads' own parts of dk and dv
+    refused(back(ws=None), "workspace", WORKSPACE)
+    refused(back(ws=P + 16), "256-byte", WORKSPACE)
+    refused(back(size=need - 1), "too small", WORKSPACE)
+    assert back(d=attention(N=0)) == 0
+
+
+@pytest.mark.parametrize("bad,word", [(dict(rows=-1), "rows"), (dict(rows=1 << 31), "rows"), (dict(dim=0), "dim"), (dict(dim=16385), "dim"), (dict(dtype=3), "dtype"),
+                                      (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"), (dict(eps=float("inf")), "eps"), (dict(dropout=-0.1), "probability"),
+                                      (dict(dropout=1.1), "probability"), (dict(dropout=float("nan")), "probability")])
+def test_norm_descriptor_refusals(bad, word):
+    lib = load_library()
+    refused(lib.rnn_add_norm_workspace_bytes(norm(**bad)), word)
+    refused(lib.rnn_add_norm_forward(norm(**bad), P, 40, None, 0, None, None, 0, P, 40, None, None), word)
+    refused(lib.rnn_add_norm_e4m3(norm(**bad), P, 40, None, 0, None, None, 0, P, 40, P, 128, None, None), word)
+    refused(lib.rnn_add_norm_backward(norm(**bad), P, 40, None, 0, P, 40, P, None, P, 40, None, 0, None, None, 0, None), word)
+
+
+def test_row_argument_refusals():
+    lib = load_library()
+    refused(lib.rnn_add_norm_forward(None, P, 40, None, 0, None, None, 0, P, 40, None, None), "descriptor")
+    refused(lib.rnn_add_norm_forward(norm(), None, 40, None, 0, None, None, 0, P, 40, None, None), "x pointer")
+    refused(lib.rnn_add_norm_forward(norm(), P, 40, None, 0, None, None, 0, None, 40, None, None), "y pointer")
+    refused(lib.rnn_add_norm_forward(norm(), P, 39, None, 0, None, None, 0, P, 40, None, None), "x: ld")
+    refused(lib.rnn_add_norm_forward(norm(), P, 40, P, 39, None, None, 0, P, 40, None, None), "residual: ld")
+    refused(lib.rnn_add_norm_forward(norm(), P, 40, None, 0, None, P, 39, P, 40, None, None), "h: ld")
+    refused(lib.rnn_add_norm_forward(norm(), P + 1, 40, None, 0, None, None, 0, P, 40, None, None), "x is not aligned")
+    refused(lib.rnn_add_norm_forward(norm(), P, 40, None, 0, P + 2, None, 0, P, 40, None, None), "gain")
+    refused(lib.rnn_add_norm_e4m3(norm(), P, 40, None, 0, None, None, 0, P, 40, P, 64, None, None), "group")
+    refused(lib.rnn_add_norm_e4m3(norm(), P, 40, None, 0, None, None, 0, P, 40, None, 0, None, None), "scales")
+    refused(lib.rnn_add_norm_backward(norm(), P, 40, None, 0, P, 40, None, None, P, 40, None, 0, None, None, 0, None), "rstd")
+    refused(lib.rnn_add_norm_backward(norm(), P, 40, None, 0, None, 40, P, None, P, 40, None, 0, None, None, 0, None), "h pointer")
+    many = norm(rows=5000)
+    need = lib.rnn_add_norm_workspace_bytes(many)
+    assert need > 0
+    refused(lib.rnn_add_norm_backward(many, P, 40, None, 0, P, 40, P, None, P, 40, None, 0, P, None, 0, None), "workspace", WORKSPACE)
+    refused(lib.rnn_add_norm_backward(many, P, 40, None, 0, P, 40, P, None, P, 40, None, 0, P, P, need - 1, None), "too small", WORKSPACE)
+    assert lib.rnn_add_norm_workspace_bytes(norm()) == 0
+    # nothing to do
+    assert lib.rnn_add_norm_forward(norm(rows=0), None, 40, None, 0, None, None, 0, None, 40, None, None) == 0
+    assert lib.rnn_add_norm_e4m3(norm(rows=0), None, 40, None, 0, None, None, 0, None, 40, None, 0, None, None) == 0
+    assert lib.rnn_add_norm_backward(norm(), P, 40, None, 0, P, 40, P, None, None, 40, None, 0, None, None, 0, None) == 0
+    refused(lib.rnn_dropout(None, P, 40, P, 40, None), "descriptor")
+    refused(lib.rnn_dropout(drop(p=1.5), P, 40, P, 40, None), "probability")
+    refused(lib.rnn_dropout(drop(dim=0), P, 40, P, 40, None), "dim")
+    refused(lib.rnn_dropout(drop(), None, 40, P, 40, None), "x pointer")
+    refused(lib.rnn_dropout(drop(), P, 40, P, 39, None), "y: ld")
+    assert lib.rnn_dropout(drop(rows=0), None, 40, None, 40, None) == 0
