@@ -68,7 +68,10 @@ struct AttnOp {
 };
 struct AttnCall { int T, N, heads, dtype; const float* log_decay; const int32_t* lengths; };
 constexpr int ATTN_MAX_DIM = 256;
-hipError_t launch_attention_steps(const AttnCall& c, const AttnOp* ops, int n_ops, hipStream_t s);
+constexpr int ATTN_STEPS = 16;      // windows of at most so many frames go frame by frame, longer ones in chunks
+// Up to three operators side by side.  space: attention_space bytes.
+int64_t attention_space(const AttnCall& c, const AttnOp* ops, int n_ops);
+hipError_t launch_attention(const AttnCall& c, const AttnOp* ops, int n_ops, float* space, hipStream_t s);
 // out (T, N, heads / group, d), of the inputs' type, = sum of `part` [T][N][heads][d] over the heads of a group.
 hipError_t launch_attention_sum_heads(const AttnCall& c, const float* part, const AttnOut& out, int d, int group, hipStream_t s);
 

@@ -85,6 +85,7 @@ int add_norm(const rnn_add_norm_desc* d, const void* x, int64_t ld_x, const void
 int check_attention(const rnn_linear_attention_desc* d) {
     if (!d) return invalid("descriptor is NULL");
     if (d->T < 0 || d->N < 0 || (int64_t)d->T * d->N >= (int64_t(1) << 31)) return invalid("attention: T and N must not be negative and T * N below 2^31");
+    if (d->T > (1 << 30)) return invalid("attention: T must not exceed 2^30");
     if (d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0) return invalid("attention: heads must be a positive multiple of kv_heads");
     if ((int64_t)d->N * d->heads >= (int64_t(1) << 20)) return invalid("attention: N * heads must be below 2^20");
     if (d->dim_k < 1 || d->dim_k > ATTN_MAX_DIM || d->dim_v < 1 || d->dim_v > ATTN_MAX_DIM) return invalid("attention: dim_k and dim_v must lie in [1, " + std::to_string(ATTN_MAX_DIM) + "]");
@@ -113,8 +114,32 @@ AttnOp forward_op(const rnn_linear_attention_desc* d, const rnn_frames* q, const
     return a;
 }
 
-// Workspace of a call: the heads' own parts of dk and dv, where several share a key / value head.
-struct AttnSpace { int64_t part_k = -1, part_v = -1, total = 0; };
+// The operators of a backward call, without their outputs: 1 dq, 2 dv, 4 dk (bits of `which`).
+int backward_ops(const rnn_linear_attention_desc* d, const AttnOp& f, const AttnTensor& t_do, int which, AttnOp* ops) {
+    int n = 0;
+    if (which & 1) {
+        AttnOp a = f;
+        a.q = t_do; a.k = f.v; a.v = f.k; a.dk = d->dim_v; a.dv = d->dim_k; a.si = 1; a.sj = d->dim_v;
+        ops[n++] = a;
+    }
+    AttnOp r = f;
+    r.reverse = true; r.early = false; r.update = d->scale; r.out = 1.0f; r.o_f32 = d->heads != d->kv_heads;
+    if (which & 2) {
+        AttnOp a = r;
+        a.q = f.k; a.k = f.q; a.v = t_do;
+        ops[n++] = a;
+    }
+    if (which & 4) {
+        AttnOp a = r;
+        a.q = f.v; a.k = t_do; a.v = f.q; a.dk = d->dim_v; a.dv = d->dim_k; a.si = 1; a.sj = d->dim_v;
+        ops[n++] = a;
+    }
+    return n;
+}
+
+// Workspace of a call: the heads' own parts of dk and dv, where several share a key / value head, and the segments' states (as many as any
+// choice of outputs takes).
+struct AttnSpace { int64_t part_k = -1, part_v = -1, segments = 0, total = 0; };
 AttnSpace space_of(const rnn_linear_attention_desc* d, bool backward) {
     AttnSpace w;
     if (backward && d->heads != d->kv_heads) {
@@ -122,6 +147,17 @@ AttnSpace space_of(const rnn_linear_attention_desc* d, bool backward) {
         w.part_k = w.total; w.total += align_up(heads * d->dim_k * 4);
         w.part_v = w.total; w.total += align_up(heads * d->dim_v * 4);
     }
+    w.segments = w.total;
+    const AttnCall c = call_of(d, nullptr, nullptr);
+    const AttnOp f = forward_op(d, nullptr, nullptr, nullptr);
+    int64_t most = 0;
+    if (!backward) most = attention_space(c, &f, 1);
+    else
+        for (int which = 1; which < 8; ++which) {
+            AttnOp ops[3];
+            most = std::max(most, attention_space(c, ops, backward_ops(d, f, f.q, which, ops)));
+        }
+    w.total += align_up(most);
     return w;
 }
 
@@ -154,7 +190,8 @@ int rnn_linear_attention_forward(const rnn_linear_attention_desc* d, const rnn_f
         AttnOp a = forward_op(d, q, k, v);
         if (with_o) a.o = output(o);
         a.s_in = d_state_in; a.s_out = d_state_out;
-        return done(launch_attention_steps(call_of(d, d_log_decay, d_lengths), &a, 1, static_cast<hipStream_t>(hip_stream)), "attention launch");
+        return done(launch_attention(call_of(d, d_log_decay, d_lengths), &a, 1, reinterpret_cast<float*>(static_cast<char*>(d_workspace) + w.segments),
+                                     static_cast<hipStream_t>(hip_stream)), "attention launch");
     });
 }
 
@@ -184,33 +221,18 @@ int rnn_linear_attention_backward(const rnn_linear_attention_desc* d, const rnn_
         const AttnCall call = call_of(d, d_log_decay, d_lengths);
         char* ws = static_cast<char*>(d_workspace);
         auto part = [&](int64_t off, int dim) { return AttnOut{ws + off, (int64_t)d->N * d->heads * dim, (int64_t)d->heads * dim, dim}; };
-        const AttnOp f = forward_op(d, q, k, v);
-        AttnTensor t_do = tensor(d_o, 1);
+        const int which = (with_q ? 1 : 0) | (with_v || d_dstate_in ? 2 : 0) | (with_k ? 4 : 0);
+        if (which == 0) return RNN_OK;
         AttnOp ops[3];
-        int n_ops = 0;
-        if (with_q) {
-            AttnOp a = f;
-            a.q = t_do; a.k = f.v; a.v = f.k; a.dk = d->dim_v; a.dv = d->dim_k; a.si = 1; a.sj = d->dim_v;
-            a.o = output(dq); a.s_in = d_state_in;
-            ops[n_ops++] = a;
+        const int n_ops = backward_ops(d, forward_op(d, q, k, v), tensor(d_o, 1), which, ops);
+        AttnOp* a = ops;
+        if (which & 1) { a->o = output(dq); a->s_in = d_state_in; ++a; }
+        if (which & 2) {
+            if (with_v) a->o = group > 1 ? part(w.part_v, d->dim_v) : output(dv);
+            a->s_in = d_dstate_out; a->s_out = d_dstate_in; ++a;
         }
-        AttnOp r = f;
-        r.reverse = true; r.early = false; r.update = d->scale; r.out = 1.0f; r.s_in = d_dstate_out; r.o_f32 = group > 1;
-        if (with_v || d_dstate_in) {
-            AttnOp a = r;
-            a.q = f.k; a.k = f.q; a.v = t_do;
-            if (with_v) a.o = group > 1 ? part(w.part_v, d->dim_v) : output(dv);
-            a.s_out = d_dstate_in;
-            ops[n_ops++] = a;
-        }
-        if (with_k) {
-            AttnOp a = r;
-            a.q = f.v; a.k = t_do; a.v = f.q; a.dk = d->dim_v; a.dv = d->dim_k; a.si = 1; a.sj = d->dim_v;
-            a.o = group > 1 ? part(w.part_k, d->dim_k) : output(dk);
-            ops[n_ops++] = a;
-        }
-        if (n_ops == 0) return RNN_OK;
-        rc = done(launch_attention_steps(call, ops, n_ops, s), "attention gradient launch");
+        if (which & 4) { a->o = group > 1 ? part(w.part_k, d->dim_k) : output(dk); a->s_in = d_dstate_out; }
+        rc = done(launch_attention(call, ops, n_ops, reinterpret_cast<float*>(ws + w.segments), s), "attention gradient launch");
         if (!rc && group > 1 && d->T > 0) {
             if (with_k) rc = done(launch_attention_sum_heads(call, (const float*)(ws + w.part_k), output(dk), d->dim_k, group, s), "attention gradient sum");
             if (!rc && with_v) rc = done(launch_attention_sum_heads(call, (const float*)(ws + w.part_v), output(dv), d->dim_v, group, s), "attention gradient sum");
