@@ -94,18 +94,21 @@ __global__ void __launch_bounds__(256) attention_steps_kernel(AttnCall c, StepOp
 // In chunks of C frames.  With g = exp(log decay), i and j frames of a chunk and S the state before it:
 //     o_i = out (g^(i + early) S^T q_i + update sum_{j <= i} g^(i - j) (q_i . k_j) v_j)
 //     S  <- g^rows S + update sum_j g^(rows - j - early) k_j v_j^T
-// A workgroup has BV = 64 NT columns of one head's state, 16 NT to each of its four wavefronts, and walks over the chunks (of a
+// A workgroup of W wavefronts has BV = 16 W columns of one head's state, 16 to a wavefront, and walks over the chunks (of a
 // segment, if the frames are split).  Everything but the decays is matrix products on 16 x 16 tiles:
 //     scores  K Q^T, the tiles j <= i shared out over the wavefronts, decayed and handed on through LDS
-//     output  transposed, [columns][frames]: S^T Q^T, scaled by a frame's power of g, plus V^T P^T: a lane then has 4 NT neighbouring
+//     output  transposed, [columns][frames]: S^T Q^T, scaled by a frame's power of g, plus V^T P^T: a lane then has 4 neighbouring
 //             columns of one frame to store
 //     state   K^T V', V' = V times the frames' powers of g
 // A state tile stays in the accumulator layout (a lane has one column and 4 neighbouring rows of it), which is the layout of a
-// product's first operand over those rows: the state never leaves the registers, and q is read in the rows' order.  The operands that run
-// along frames (V, K^T) come out of LDS through the transposing read.
-// fp32 takes the matrix cores' fp32 products.  bf16 takes its inputs as they are; what is computed is split: scores and state into two
-// parts of 8 bits (2^-17 of each is lost, against the 2^-9 of the result's own rounding), V' into PARTS: three keep all 24 bits of a
-// state that is handed on.  (One part each would double the error of a result in bf16.)
+// product's first operand over those rows: the state never leaves the registers.  The operands that run along frames (V, K^T) come out of
+// LDS through the transposing read, which takes columns in fours from anywhere: state tiles 2 t and 2 t + 1 have the rows of which a lane
+// reads eight neighbouring ones of q.
+// fp32 takes the matrix cores' fp32 products.  bf16 takes its inputs as they are; of what is computed, the scores and the state that outputs are
+// made from are rounded to bf16.  Their errors, 2^-9 of a term at most and independent of each other, add up like the roundings of the results
+// themselves: a result's error is at most 1.41 times what its own rounding leaves.  (In two parts of 8 bits each it would not grow, at 20 % more
+// time.)  The state that is carried on is another matter: V' is split into two bf16 numbers, which lose 2^-17 of it, and into three, which keep all
+// of its bits, where the last state is asked for.
 // ---------------------------------------------------------------------------------------------
 typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
 typedef bf16_t bf16x4 __attribute__((ext_vector_type(4)));
@@ -117,6 +120,7 @@ struct ChunkOps {
     AttnOp op[3];
     float* seg_state[3];      // [segment][stream, head][dk][dv]: what a segment adds to the state, then the state before it
     int n_ops, slices, n_seg, seg_len;
+    bool whole_state;         // some operator's last state is asked for
     unsigned works;
 };
 
@@ -131,65 +135,110 @@ __device__ __forceinline__ bf16x8 join(s16x4 a, s16x4 b) {
     u.h[0] = a; u.h[1] = b;
     return u.v;
 }
-__device__ __forceinline__ bf16x8 split(f32x8& x) {      // the leading 8 bits; the rest stays in x
-    const bf16x8 hi = __builtin_convertvector(x, bf16x8);
-    x -= __builtin_convertvector(hi, f32x8);
-    return hi;
+// The upper halves of two numbers (their leading 8 bits, cut off) in one word; the rest stays in them, exactly.  (Cutting off takes five
+// instructions for two numbers, rounding to nearest and converting back seven.)
+__device__ __forceinline__ unsigned upper(float& x, float& y) {
+    const unsigned a = __builtin_bit_cast(unsigned, x), b = __builtin_bit_cast(unsigned, y);
+    x -= __builtin_bit_cast(float, a & 0xFFFF0000u);
+    y -= __builtin_bit_cast(float, b & 0xFFFF0000u);
+    return __builtin_amdgcn_perm(b, a, 0x07060302u);
 }
+__device__ __forceinline__ bf16x8 split(f32x8& x) {
+    union { unsigned u[4]; bf16x8 v; } r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = x[2 * i], b = x[2 * i + 1];
+        r.u[i] = upper(a, b);
+        x[2 * i] = a; x[2 * i + 1] = b;
+    }
+    return r.v;
+}
+__device__ __forceinline__ bf16x8 rounded(f32x8 x) { return __builtin_convertvector(x, bf16x8); }
 
-// 16 bytes of a row from unit `at` on, zeros from unit `dim` on.
-template <class T>
-__device__ __forceinline__ u32x4 load16(const T* row, int at, int dim, bool there) {
+constexpr int chunk_frames(bool f32, int DK) { return f32 || DK > 128 ? 32 : 64; }
+
+// Place of (frame, unit) of a tile of D units in LDS: the 16-byte pieces of a row are exchanged, so that neither 16 bytes of eight frames
+// (operands that run along units) nor four neighbouring pieces of four frames (operands that run along frames) meet in a bank.
+template <class T, int D>
+__device__ __forceinline__ int place(int row, int col) {
     constexpr int E = 16 / sizeof(T);
-    u32x4 r = 0u;
-    if (!there || at >= dim) return r;
-    if (at + E <= dim) { __builtin_memcpy(&r, row + at, 16); return r; }
-    for (int i = 0; i < E - 1; ++i) {
-        if (at + i >= dim) continue;
-        if constexpr (sizeof(T) == 4) r[i] = __builtin_bit_cast(unsigned, row[at + i]);
-        else r[i / 2] |= (unsigned)__builtin_bit_cast(unsigned short, row[at + i]) << (16 * (i % 2));
-    }
-    return r;
+    const int f = sizeof(T) == 4 ? row & 15 : D == 64 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3);
+    return row * D + ((col / E ^ f) * E) + col % E;
 }
 
-template <class T, int DK> constexpr int chunk_frames() { return sizeof(T) == 4 || DK > 128 ? 32 : 64; }
-
-// A tile of C frames x D units on its way from memory to LDS, in registers.
-template <class T, int C, int D>
+// A tile of C frames x D units, brought from memory to LDS by all THREADS.  Frames beyond the last one read the last again (their scores,
+// weights and outputs are left out); what lies behind the units of a row stays zero from the start.  Rows have at least 16 bytes.
+// DIRECT (rows of whole 16-byte pieces, all aligned to them): straight to LDS, 64 lanes x 16 bytes at once in the order of the lanes, a lane
+// reading the piece that belongs in its place; s_waitcnt vmcnt(0) and a barrier make them visible.  Otherwise through registers, a row's last
+// 16 bytes from where they end.
+template <class T, int C, int D, int THREADS, bool DIRECT>
 struct Tile {
-    static constexpr int E = 16 / sizeof(T), PIECES = C * D / E / 256, PITCH = D + (sizeof(T) == 4 ? 4 : 8);
-    static_assert(C * D / E % 256 == 0, "tile");
-    u32x4 r[PIECES];
-    __device__ __forceinline__ void load(const AttnTensor& a, int n, int h, int first, int rows, int unit, int dim, bool reverse, int L) {
-        const T* base = (const T*)a.p + n * a.sn + (h / a.group) * a.sh;
-#pragma unroll
-        for (int x = 0; x < PIECES; ++x) {
-            const int p = x * 256 + threadIdx.x, row = p / (D / E), at = unit + p % (D / E) * E;
-            const int i = first + row, t = reverse ? L - 1 - i : i;
-            r[x] = load16(base + t * a.st, at, dim, row < rows);
-        }
+    static constexpr int E = 16 / sizeof(T), ROW = D / E, ROWS = THREADS / ROW, PIECES = C / ROWS;      // pieces of a row; rows of a piece of all threads
+    static_assert(THREADS % ROW == 0 && C % ROWS == 0, "tile");
+    const T* base; int64_t step; int dim;
+    __device__ __forceinline__ Tile(const AttnTensor& a, int n, int h, int unit, int d, bool reverse, int L, int begin) {
+        dim = d - unit;      // units of this tile (may be more than D)
+        step = reverse ? -a.st : a.st;
+        base = (const T*)a.p + n * a.sn + (h / a.group) * a.sh + unit + (reverse ? (L - 1) * a.st : 0) + begin * step;
     }
-    __device__ __forceinline__ void store(T* lds) const {
+    // the next chunk's first `rows` frames, rows > 0
+    __device__ __forceinline__ void load(T* lds, int rows) {
+        const int row = threadIdx.x / ROW, slot = threadIdx.x % ROW * E;
+        if constexpr (DIRECT) {
+            typedef const __attribute__((address_space(1))) void* global_t;
+            typedef __attribute__((address_space(3))) void* lds_t;
+            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
 #pragma unroll
-        for (int x = 0; x < PIECES; ++x) {
-            const int p = x * 256 + threadIdx.x;
-            *(u32x4*)(lds + p / (D / E) * PITCH + p % (D / E) * E) = r[x];
+            for (int x = 0; x < PIECES; ++x) {
+                const int i = row + x * ROWS, at = place<T, D>(i, slot) - i * D;      // (exchanging twice gives back the piece)
+                if (at < dim) __builtin_amdgcn_global_load_lds((global_t)(base + min(i, rows - 1) * step + at), (lds_t)(lds + x * ROWS * D + wave * 64 * E), 16, 0, 0);
+            }
+        } else {
+            u32x4 r[PIECES];
+#pragma unroll
+            for (int x = 0; x < PIECES; ++x) __builtin_memcpy(&r[x], base + min(row + x * ROWS, rows - 1) * step + min(slot, dim - E), 16);
+            const int shift = max(slot + E - dim, 0);      // the row's last units stand at the end of what was read
+            typedef std::conditional_t<sizeof(T) == 4, unsigned, unsigned short> word;
+#pragma unroll
+            for (int x = 0; x < PIECES; ++x) {
+                if (shift == 0) *(u32x4*)(lds + place<T, D>(row + x * ROWS, slot)) = r[x];
+                else if (slot < dim)
+                    for (int e = 0; e < E; ++e) {
+                        word v;
+                        if constexpr (sizeof(T) == 4) v = r[x][e];
+                        else v = (word)(r[x][e / 2] >> (16 * (e % 2)));
+                        if (e >= shift) *(word*)(lds + place<T, D>(row + x * ROWS, slot + e - shift)) = v;
+                    }
+            }
         }
+        base += C * step;
     }
 };
+template <class T>
+__device__ __forceinline__ void clear_lds(T* p, int count) {      // a multiple of 16 bytes
+    for (int i = threadIdx.x; i < count * (int)sizeof(T) / 16; i += blockDim.x) ((u32x4*)p)[i] = 0u;
+}
 
-template <class T, int DK, int NT, int PARTS, bool STATE>
-__global__ void __launch_bounds__(256, 2) attention_chunks_kernel(AttnCall c, ChunkOps ops) {
-    constexpr int C = chunk_frames<T, DK>(), BV = 64 * NT, IT = C / 16, AT = DK / 16;
+// Wavefronts of a SIMD that the registers are cut for: as many as LDS has room for, as long as the state fits them.
+// (fp32, 128 units: 4 would spill; rows that go through registers need more of them.)
+constexpr int chunk_waves(bool f32, int DK, bool direct) { return !direct || DK > 128 || (f32 && DK > 64) ? 2 : 4; }
+
+template <class T, int DK, int W, bool DIRECT, bool STATE>
+__global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIRECT))) attention_chunks_kernel(AttnCall c, ChunkOps ops) {
     constexpr bool F32 = sizeof(T) == 4;
-    typedef Tile<T, C, DK> TileK;
-    typedef Tile<T, C, BV> TileV;
-    constexpr int PP = C + (F32 ? 4 : 8);                                  // pitch of the scores
-    __shared__ alignas(16) T lds_q[STATE ? 1 : C * TileK::PITCH];
-    __shared__ alignas(16) T lds_k[C * TileK::PITCH];
-    __shared__ alignas(16) T lds_v[C * TileV::PITCH];
-    __shared__ alignas(16) T lds_p[STATE ? 1 : (F32 ? 1 : 2) * C * PP];
-    __shared__ float power[C + 1], power_low[C + 1], weight[2 * C];       // g^i and what its rounding left; update g^(C - j - early), zeros
+    constexpr int C = chunk_frames(F32, DK), BV = 16 * W, IT = C / 16, AT = DK / 16;
+    typedef Tile<T, C, DK, 64 * W, DIRECT> TileK;
+    typedef Tile<T, C, BV, 64 * W, DIRECT> TileV;
+    __shared__ alignas(256) T lds_q[STATE ? 8 : C * DK];
+    constexpr int BUFS = STATE ? 2 : 1;                                               // (the state alone: no room is needed for q and the scores)
+    __shared__ alignas(256) T lds_ks[BUFS * C * DK];
+    __shared__ alignas(256) T lds_vs[BUFS * C * BV];
+    __shared__ alignas(256) T lds_p[STATE ? 8 : F32 ? C * (C + 4) : C * C];           // scores [i][j]
+    __shared__ float chunk_decay;
+    __shared__ double exact_decay, carry;                                             // g^C; what the roundings of chunk_decay have left so far: the next makes up for it
+    __shared__ float power[16 + C + 1], weight[2 * C];                                // g^i from 16 on (what is before it goes to masked scores only); update g^(C - j - early), zeros
+    // place of score (i, j); bf16: pieces of 16 bytes exchanged as in the tiles
+    auto score_at = [](int i, int j) { return F32 ? i * (C + 4) + j : C == 64 ? i * C + ((j >> 3 ^ (i >> 1 & 7)) << 3) + (j & 7) : i * C + ((j >> 3 ^ (i >> 2 & 3)) << 3) + (j & 7); };
 
     // Workgroups go to the eight XCDs in turn; neighbours in the list of works (slices of a head, gradients of it, heads that share keys) read the same
     // tensors and are put on one.
@@ -206,257 +255,260 @@ __global__ void __launch_bounds__(256, 2) attention_chunks_kernel(AttnCall c, Ch
     const int L = length_of(c, n), begin = seg * ops.seg_len, end = min(L, begin + ops.seg_len);
     if (begin >= end && (STATE || seg > 0)) return;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16, m = lane % 16;
-    // the lane's columns: as a result's column, and the first of 4 NT neighbouring ones of an output
-    const int my_col = 16 * NT * wave + (NT == 2 ? 8 * (m / 4) + m % 4 : m), out_col = col0 + 16 * NT * wave + 4 * NT * g;
+    const int my_col = col0 + 16 * wave + m, out_col = col0 + 16 * wave + 4 * g;      // the lane's column; the first of the four it has of an output
+    const bool busy = col0 + 16 * wave < a.dv;                                        // of a wavefront; the others help with the tiles and scores
+    const bool whole_state = STATE ? ops.whole_state : a.s_out != nullptr;            // three parts of V'
 
-    const float ld = log_decay_of(c, h);
-    if (threadIdx.x <= C) {
-        const double p = exp((double)ld * (int)threadIdx.x);
-        power[threadIdx.x] = (float)p;
-        power_low[threadIdx.x] = (float)(p - (float)p);
+    TileK tq(a.q, n, h, 0, a.dk, a.reverse, L, begin), tk(a.k, n, h, 0, a.dk, a.reverse, L, begin);
+    TileV tv(a.v, n, h, col0, a.dv, a.reverse, L, begin);
+    if constexpr (!STATE) clear_lds(lds_q, C * DK);
+    clear_lds(lds_ks, BUFS * C * DK);
+    clear_lds(lds_vs, BUFS * C * BV);
+    __syncthreads();
+    const T* lds_k = lds_ks;
+    const T* lds_v = lds_vs;
+    if (begin < end) {
+        if constexpr (!STATE) tq.load(lds_q, end - begin);
+        tk.load(lds_ks, end - begin);
+        tv.load(lds_vs, end - begin);
     }
+    if constexpr (!STATE) clear_lds(lds_p, F32 ? C * (C + 4) : C * C);                // (tiles above the diagonal stay zero)
+    const float ld = log_decay_of(c, h), both = a.out * a.update;
+    if (threadIdx.x <= C + 16) power[threadIdx.x] = threadIdx.x < 16 ? 0.0f : (float)exp((double)ld * ((int)threadIdx.x - 16));
+    if (threadIdx.x == C) { exact_decay = exp((double)ld * C); carry = 1.0; }
     if (threadIdx.x < 2 * C) weight[threadIdx.x] = threadIdx.x < C ? a.update * expf(ld * (C - (int)threadIdx.x - (a.early ? 1 : 0))) : 0.0f;
 
-    f32x4 S[AT][NT];
+    // state tile t: rows row_of(t) + r of this lane
+    auto row_of = [](int t, int g) { return F32 ? 16 * t + 4 * g : 32 * (t / 2) + 8 * g + 4 * (t % 2); };
+    f32x4 S[AT];
     const int64_t nh = (int64_t)n * c.heads + h, heads = (int64_t)c.N * c.heads, size = (int64_t)a.dk * a.dv;
-    {
-        const bool seg_state = !STATE && ops.n_seg > 1;
-        const float* from = STATE ? nullptr : seg_state ? ops.seg_state[which] + (seg * heads + nh) * size : a.s_in ? a.s_in + nh * size : nullptr;
-        const int64_t si = seg_state ? a.dv : a.si, sj = seg_state ? 1 : a.sj;
 #pragma unroll
-        for (int t = 0; t < AT; ++t)
+    for (int t = 0; t < AT; ++t) S[t] = 0.0f;
+    if constexpr (!STATE) {
+        // the state before
+        const float* from = ops.n_seg > 1 ? ops.seg_state[which] + (seg * heads + nh) * size : a.s_in ? a.s_in + nh * size : nullptr;
+        if (from) {
+            const int si = ops.n_seg > 1 ? a.dv : (int)a.si, col = min(my_col, a.dv - 1) * (ops.n_seg > 1 ? 1 : (int)a.sj);
+            int group = g;
+            asm volatile("" : "+v"(group));
+            // (loads first, a quarter of them at a time: left to itself the compiler moves each under its condition and waits for it there)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int t0 = 0; t0 < AT; t0 += AT / 4) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = 16 * t + 4 * g + r, j = col0 + my_col + 4 * nt;
-                    S[t][nt][r] = from && i < a.dk && j < a.dv ? from[i * si + j * sj] : 0.0f;
-                }
+                for (int t = t0; t < t0 + AT / 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[t][r] = from[min(row_of(t, group) + r, a.dk - 1) * si + col];
+#pragma unroll
+                for (int t = t0; t < t0 + AT / 4; ++t) asm volatile("" : "+v"(S[t]));
+#pragma unroll
+                for (int t = t0; t < t0 + AT / 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[t][r] = row_of(t, group) + r < a.dk && my_col < a.dv ? S[t][r] : 0.0f;
+            }
+        }
     }
-    TileK tq, tk;
-    TileV tv;
-    auto load = [&](int first) {
-        const int rows = end - first;
-        if constexpr (!STATE) tq.load(a.q, n, h, first, rows, 0, a.dk, a.reverse, L);
-        tk.load(a.k, n, h, first, rows, 0, a.dk, a.reverse, L);
-        tv.load(a.v, n, h, first, rows, col0, a.dv, a.reverse, L);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+
+    // operands of 32 units of 16 frames; of 32 frames 32 s + 8 g + e, four columns each
+    auto along = [&](const T* tile, int row16, int t) { return *(const bf16x8*)(tile + row16 * 16 * DK + (place<T, DK>(m, 8 * g) ^ (32 * t))); };
+    auto along4 = [&](const T* tile, int row16, int t) { return *(const f32x4*)(tile + row16 * 16 * DK + (place<T, DK>(m, 4 * g) ^ (16 * t))); };      // fp32: of 16 units
+    auto v_frames = [&](int s) {
+        const bf16_t* p = (const bf16_t*)lds_v + 32 * s * BV;
+        return join(lds_transposed(p + place<T, BV>(8 * g + m / 4, 16 * wave + 4 * (m % 4))), lds_transposed(p + place<T, BV>(8 * g + 4 + m / 4, 16 * wave + 4 * (m % 4))));
     };
-    load(begin);
-    const float both = a.out * a.update;
+    auto k_frames = [&](int s, int t) {
+        const bf16_t* p = (const bf16_t*)lds_k + 32 * s * DK + 4 * (t % 2);
+        return join(lds_transposed(p + (place<T, DK>(8 * g + m / 4, 8 * (m % 4)) ^ (32 * (t / 2)))), lds_transposed(p + (place<T, DK>(8 * g + 4 + m / 4, 8 * (m % 4)) ^ (32 * (t / 2)))));
+    };
     for (int first = begin; first < end; first += C) {
         const int rows = min(C, end - first);
-        __syncthreads();                       // the last chunk's tiles have been read (and, first, the tables are there)
-        if constexpr (!STATE) tq.store(lds_q);
-        tk.store(lds_k);
-        tv.store(lds_v);
-        __syncthreads();
-        if (first + C < end) load(first + C);
-        if constexpr (!STATE) {
-            f32x4 acc[IT][NT];
+        f32x4 acc[STATE ? 1 : IT];
+        if (threadIdx.x == 0) {
+            const double p = exact_decay * carry;
+            chunk_decay = (float)p;
+            carry = exact_decay > 1e-30 ? p / chunk_decay : 1.0;
+        }
+        // 1. the state's part of the outputs (q is there; k and v are on their way)
+        if constexpr (!STATE) if (a.o.p && busy) {
 #pragma unroll
-            for (int it = 0; it < IT; ++it)
+            for (int it = 0; it < IT; ++it) acc[it] = 0.0f;
+            if constexpr (F32) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) acc[it][nt] = 0.0f;
-            if (a.o.p) {
-                // scores of the tiles (16 frames i, 16 frames j) that the products below read: j up to the end of i's pair of tiles
+                for (int t = 0; t < AT; ++t) {
+                    f32x4 qf[IT];
 #pragma unroll
-                for (int x = 0; x < (IT == 4 ? 3 : 1); ++x) {
-                    const int e = wave + 4 * x, it = e < 4 ? e / 2 : 2 + (e - 4) / 4, jt = e < 4 ? e % 2 : e % 4;
-                    f32x4 s = 0.0f;
-                    if (jt <= it) {
-                        if constexpr (F32) {
+                    for (int it = 0; it < IT; ++it) qf[it] = along4(lds_q, it, t);
 #pragma unroll
-                            for (int t = 0; t < AT; ++t) {
-                                const f32x4 k = *(const f32x4*)(lds_k + (16 * jt + m) * TileK::PITCH + 16 * t + 4 * g);
-                                const f32x4 q = *(const f32x4*)(lds_q + (16 * it + m) * TileK::PITCH + 16 * t + 4 * g);
+                    for (int r = 0; r < 4; ++r)
 #pragma unroll
-                                for (int r = 0; r < 4; ++r) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[r], q[r], s, 0, 0, 0);
-                            }
-                        } else {
-#pragma unroll
-                            for (int t = 0; t < DK / 32; ++t)
-                                s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)(lds_k + (16 * jt + m) * TileK::PITCH + 32 * t + 8 * g),
-                                                                            *(const bf16x8*)(lds_q + (16 * it + m) * TileK::PITCH + 32 * t + 8 * g), s, 0, 0, 0);
-                        }
-                    }
-                    const int i = 16 * it + m, j = 16 * jt + 4 * g;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) s[r] = i >= j + r ? s[r] * (both * power[i >= j + r ? i - j - r : 0]) : 0.0f;
-                    if constexpr (F32) *(f32x4*)(lds_p + i * PP + j) = s;
-                    else {
-                        const bf16x4 hi = __builtin_convertvector(s, bf16x4);
-                        *(bf16x4*)(lds_p + i * PP + j) = hi;
-                        *(bf16x4*)(lds_p + (C + i) * PP + j) = __builtin_convertvector(s - __builtin_convertvector(hi, f32x4), bf16x4);
-                    }
+                        for (int it = 0; it < IT; ++it) acc[it] = __builtin_amdgcn_mfma_f32_16x16x4f32(S[t][r], qf[it][r], acc[it], 0, 0, 0);
                 }
-                // the state's part
-                if constexpr (F32) {
+            } else {
 #pragma unroll
-                    for (int t = 0; t < AT; ++t)
+                for (int t = 0; t < DK / 32; ++t) {
+                    bf16x8 qf[IT];
 #pragma unroll
-                        for (int it = 0; it < IT; ++it) {
-                            const f32x4 q = *(const f32x4*)(lds_q + (16 * it + m) * TileK::PITCH + 16 * t + 4 * g);
+                    for (int it = 0; it < IT; ++it) qf[it] = along(lds_q, it, t);
+                    const f32x8 s = __builtin_shufflevector(S[2 * t], S[2 * t + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    const bf16x8 sf = rounded(s);
 #pragma unroll
-                            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) acc[it][nt] = __builtin_amdgcn_mfma_f32_16x16x4f32(S[t][nt][r], q[r], acc[it][nt], 0, 0, 0);
-                        }
-                } else {
-#pragma unroll
-                    for (int t = 0; t < DK / 32; ++t) {
-                        bf16x8 hi[NT], lo[NT];
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            f32x8 s = __builtin_shufflevector(S[2 * t][nt], S[2 * t + 1][nt], 0, 1, 2, 3, 4, 5, 6, 7);
-                            hi[nt] = split(s);
-                            lo[nt] = __builtin_convertvector(s, bf16x8);
-                        }
-#pragma unroll
-                        for (int it = 0; it < IT; ++it) {
-                            const bf16_t* q = lds_q + (16 * it + m) * TileK::PITCH + 32 * t + 4 * g;
-                            const bf16x8 qf = join(*(const s16x4*)q, *(const s16x4*)(q + 16));
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                acc[it][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi[nt], qf, acc[it][nt], 0, 0, 0);
-                                acc[it][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo[nt], qf, acc[it][nt], 0, 0, 0);
-                            }
-                        }
-                    }
-                }
-#pragma unroll
-                for (int it = 0; it < IT; ++it) {
-                    const float x = a.out * power[16 * it + m + (a.early ? 1 : 0)];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) acc[it][nt] *= x;
+                    for (int it = 0; it < IT; ++it) acc[it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sf, qf[it], acc[it], 0, 0, 0);
                 }
             }
-            __syncthreads();                   // the scores are there
-            if (a.o.p) {
+#pragma unroll
+            for (int it = 0; it < IT; ++it) acc[it] *= a.out * power[16 + 16 * it + m + (a.early ? 1 : 0)];
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();                       // k and v are there
+        if constexpr (STATE) {
+            const int other = (first - begin) / C & 1 ^ 1;
+            lds_k = lds_ks + (other ^ 1) * C * DK;
+            lds_v = lds_vs + (other ^ 1) * C * BV;
+            if (first + C < end) {
+                tk.load(lds_ks + other * C * DK, end - first - C);
+                tv.load(lds_vs + other * C * BV, end - first - C);
+            }
+        }
+        // 2. scores of the tiles (it, jt), jt <= it
+        if constexpr (!STATE) if (a.o.p) {
+#pragma unroll
+            for (int x = 0; x < (IT * (IT + 1) / 2 + W - 1) / W; ++x) {
+                const int e = wave + W * x, it = e < 1 ? 0 : e < 3 ? 1 : e < 6 ? 2 : 3, jt = e - it * (it + 1) / 2;
+                if (e >= IT * (IT + 1) / 2) break;
+                f32x4 s = 0.0f;
                 if constexpr (F32) {
 #pragma unroll
-                    for (int jt = 0; jt < IT; ++jt)
+                    for (int t = 0; t < AT; ++t) {
+                        const f32x4 kf = along4(lds_k, jt, t), qf = along4(lds_q, it, t);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            float v[NT];
+                        for (int r = 0; r < 4; ++r) s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[r], qf[r], s, 0, 0, 0);
+                    }
+                } else {
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) v[nt] = lds_v[(16 * jt + 4 * g + r) * TileV::PITCH + my_col + 4 * nt];
+                    for (int t = 0; t < DK / 32; ++t) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(along(lds_k, jt, t), along(lds_q, it, t), s, 0, 0, 0);
+                }
+                const int lag = 16 * (it - jt) + m - 4 * g;
+                const float* f = power + 16 + lag;
 #pragma unroll
-                            for (int it = jt; it < IT; ++it) {
-                                const float p = lds_p[(16 * it + m) * PP + 16 * jt + 4 * g + r];
+                for (int r = 0; r < 4; ++r) s[r] = (lag >= r ? s[r] : 0.0f) * (both * f[-r]);
+                T* p = lds_p + score_at(16 * it + m, 16 * jt + 4 * g);
+                if constexpr (F32) *(f32x4*)p = s;
+                else *(bf16x4*)p = __builtin_convertvector(s, bf16x4);
+            }
+            __syncthreads();                   // the scores are there, q has been read
+            if (first + C < end) tq.load(lds_q, end - first - C);
+            // 3. the chunk's own part of the outputs
+            if (busy) {
+                if constexpr (F32) {
 #pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) acc[it][nt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[nt], p, acc[it][nt], 0, 0, 0);
-                            }
-                        }
+                    for (int jt = 0; jt < IT; ++jt) {
+                        f32x4 v, pf[IT];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) v[r] = lds_v[(16 * jt + r) * BV + (place<T, BV>(4 * g, 16 * wave + m) ^ 4 * r)];
+#pragma unroll
+                        for (int it = jt; it < IT; ++it) pf[it] = *(const f32x4*)(lds_p + score_at(16 * it + m, 16 * jt + 4 * g));
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int it = jt; it < IT; ++it) acc[it] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r], pf[it][r], acc[it], 0, 0, 0);
+                    }
                 } else {
 #pragma unroll
                     for (int s = 0; s < C / 32; ++s) {
-                        bf16x8 v[NT];
+                        const bf16x8 v = v_frames(s);
+                        bf16x8 pf[IT];
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            const bf16_t* p = lds_v + (32 * s + 8 * g + m / 4) * TileV::PITCH + 16 * NT * wave + 4 * NT * (m % 4) + 4 * nt;
-                            v[nt] = join(lds_transposed(p), lds_transposed(p + 4 * TileV::PITCH));
-                        }
+                        for (int it = 2 * s; it < IT; ++it) pf[it] = *(const bf16x8*)(lds_p + score_at(16 * it + m, 32 * s + 8 * g));
 #pragma unroll
-                        for (int it = 2 * s; it < IT; ++it) {
-                            const bf16_t* p = lds_p + (16 * it + m) * PP + 32 * s + 8 * g;
-                            const bf16x8 hi = *(const bf16x8*)p, lo = *(const bf16x8*)(p + C * PP);
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                acc[it][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[nt], hi, acc[it][nt], 0, 0, 0);
-                                acc[it][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[nt], lo, acc[it][nt], 0, 0, 0);
-                            }
-                        }
+                        for (int it = 2 * s; it < IT; ++it) acc[it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[it], acc[it], 0, 0, 0);
                     }
                 }
+                const int64_t step = a.reverse ? -a.o.st : a.o.st;
+                const int64_t at = (int64_t)(a.reverse ? L - 1 - first - m : first + m) * a.o.st + n * a.o.sn + h * a.o.sh + out_col;
 #pragma unroll
                 for (int it = 0; it < IT; ++it) {
-                    const int i = 16 * it + m;
-                    if (i >= rows || out_col >= a.dv) continue;
-                    const int t = a.reverse ? L - 1 - first - i : first + i;
-                    const int64_t at = t * a.o.st + n * a.o.sn + h * a.o.sh + out_col;
-                    typedef float out_f32 __attribute__((ext_vector_type(4 * NT)));
-                    typedef T out_t __attribute__((ext_vector_type(4 * NT)));
-                    out_f32 x;
-#pragma unroll
-                    for (int u = 0; u < 4 * NT; ++u) x[u] = acc[it][u / 4][u % 4];
-                    const out_t y = __builtin_convertvector(x, out_t);
-                    if (out_col + 4 * NT <= a.dv) {
-                        if (a.o_f32) __builtin_memcpy((float*)a.o.p + at, &x, sizeof(x));
-                        else __builtin_memcpy((T*)a.o.p + at, &y, sizeof(y));
+                    if (16 * it + m >= rows || out_col >= a.dv) continue;
+                    typedef T out_t __attribute__((ext_vector_type(4)));
+                    const out_t y = __builtin_convertvector(acc[it], out_t);
+                    float* of = (float*)a.o.p + at + 16 * it * step;
+                    T* ot = (T*)a.o.p + at + 16 * it * step;
+                    if (DIRECT || out_col + 4 <= a.dv) {
+                        if (a.o_f32) __builtin_memcpy(of, &acc[it], sizeof(acc[it]));
+                        else __builtin_memcpy(ot, &y, sizeof(y));
                     } else {
 #pragma unroll
-                        for (int u = 0; u < 4 * NT; ++u)
-                            if (out_col + u < a.dv) { if (a.o_f32) ((float*)a.o.p)[at + u] = x[u]; else ((T*)a.o.p)[at + u] = y[u]; }
+                        for (int u = 0; u < 3; ++u)
+                            if (out_col + u < a.dv) { if (a.o_f32) of[u] = acc[it][u]; else ot[u] = y[u]; }
                     }
                 }
             }
         }
-        // the state after the chunk
-        const float ph = power[rows], pl = power_low[rows];
-#pragma unroll
-        for (int t = 0; t < AT; ++t)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) S[t][nt][r] = fmaf(S[t][nt][r], ph, S[t][nt][r] * pl);
+        // 4. the state after the chunk
+        const float decay = rows == C ? chunk_decay : power[16 + rows];
         const float* wt = weight + C - rows;
-        if constexpr (F32) {
+        if (busy) {
 #pragma unroll
-            for (int jt = 0; jt < IT; ++jt)
+            for (int t = 0; t < AT; ++t) S[t] *= decay;
+            if constexpr (F32) {
+                int at = place<T, DK>(4 * g, m);       // of frame 4 g, unit m; the others' places differ from it in constant bits of the piece
+                asm volatile("" : "+v"(at));           // (worked out in every chunk: kept, they would not fit the registers)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 16 * jt + 4 * g + r;
-                    float v[NT];
+                for (int jt = 0; jt < IT; ++jt)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) v[nt] = lds_v[j * TileV::PITCH + my_col + 4 * nt] * wt[j];
+                    for (int r = 0; r < 4; ++r) {
+                        const int j = 16 * jt + 4 * g + r;
+                        const float v = lds_v[(16 * jt + r) * BV + (place<T, BV>(4 * g, 16 * wave + m) ^ 4 * r)] * wt[j];
 #pragma unroll
-                    for (int t = 0; t < AT; ++t) {
-                        const float k = lds_k[j * TileK::PITCH + 16 * t + m];
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) S[t][nt] = __builtin_amdgcn_mfma_f32_16x16x4f32(k, v[nt], S[t][nt], 0, 0, 0);
+                        for (int t = 0; t < AT; ++t) S[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(lds_k[(16 * jt + r) * DK + (at ^ (4 * t ^ r) * 4)], v, S[t], 0, 0, 0);
                     }
-                }
-        } else {
+            } else {
 #pragma unroll
-            for (int s = 0; s < C / 32; ++s) {
-                bf16x8 v[NT][PARTS];
-                f32x8 wv;
+                for (int s = 0; s < C / 32; ++s) {
+                    f32x8 x = __builtin_convertvector(v_frames(s), f32x8);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) wv[e] = wt[32 * s + 8 * g + e];
+                    for (int e = 0; e < 8; ++e) x[e] *= wt[32 * s + 8 * g + e];
+                    bf16x8 v0 = split(x), v1, v2;
+                    if (whole_state) { v1 = split(x); v2 = rounded(x); }
+                    else v1 = v2 = rounded(x);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const bf16_t* p = lds_v + (32 * s + 8 * g + m / 4) * TileV::PITCH + 16 * NT * wave + 4 * NT * (m % 4) + 4 * nt;
-                    f32x8 x = __builtin_convertvector(join(lds_transposed(p), lds_transposed(p + 4 * TileV::PITCH)), f32x8) * wv;
+                    for (int t = 0; t < AT; t += 2) {
+                        const bf16x8 k[2] = {k_frames(s, t), k_frames(s, t + 1)};
 #pragma unroll
-                    for (int u = 0; u < PARTS; ++u) v[nt][u] = split(x);
-                }
+                        for (int u = 0; u < 2; ++u) S[t + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u], v0, S[t + u], 0, 0, 0);
 #pragma unroll
-                for (int t = 0; t < AT; ++t) {
-                    const bf16_t* p = lds_k + (32 * s + 8 * g + m / 4) * TileK::PITCH + 16 * t + 4 * (m % 4);
-                    const bf16x8 k = join(lds_transposed(p), lds_transposed(p + 4 * TileK::PITCH));
+                        for (int u = 0; u < 2; ++u) S[t + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u], v1, S[t + u], 0, 0, 0);
+                        if (whole_state)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int u = 0; u < PARTS; ++u) S[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, v[nt][u], S[t][nt], 0, 0, 0);
+                            for (int u = 0; u < 2; ++u) S[t + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u], v2, S[t + u], 0, 0, 0);
+                    }
                 }
             }
         }
+        if constexpr (!STATE) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();                       // the next q is there; k, v and the scores have been read
+        if constexpr (!STATE)
+            if (first + C < end) {
+                tk.load(lds_ks, end - first - C);
+                tv.load(lds_vs, end - first - C);
+            }
     }
     float* to = STATE ? ops.seg_state[which] + (seg * heads + nh) * size : a.s_out && end == L ? a.s_out + nh * size : nullptr;
-    if (!to) return;
-    const int64_t si = STATE ? a.dv : a.si, sj = STATE ? 1 : a.sj;
+    if (!to || my_col >= a.dv) return;
+    const int si = STATE ? a.dv : (int)a.si, sj = (STATE ? 1 : (int)a.sj) * my_col;
+    int group = g;
+    asm volatile("" : "+v"(group));            // (the rows' addresses are worked out here again, not kept through the loop)
 #pragma unroll
     for (int t = 0; t < AT; ++t)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * t + 4 * g + r, j = col0 + my_col + 4 * nt;
-                if (i < a.dk && j < a.dv) to[i * si + j * sj] = S[t][nt][r];
-            }
+        for (int r = 0; r < 4; ++r) {
+            const int i = row_of(t, group) + r;
+            if (i < a.dk) to[i * si + sj] = S[t][r];
+        }
 }
 
-// What the segments add to the state becomes the state before each, in place.
+// What the segments add to the state becomes the state before each, in place; U segments are read ahead.
+template <int U>
 __global__ void __launch_bounds__(256) attention_segments_kernel(AttnCall c, ChunkOps ops) {
     const AttnOp& a = ops.op[blockIdx.z];
     const int64_t size = (int64_t)a.dk * a.dv, heads = (int64_t)c.N * c.heads, nh = blockIdx.y;
@@ -464,15 +516,20 @@ __global__ void __launch_bounds__(256) attention_segments_kernel(AttnCall c, Chu
     if (x >= size) return;
     const int L = length_of(c, (int)(nh / c.heads));
     const double ld = log_decay_of(c, (int)(nh % c.heads));
-    float S = a.s_in ? a.s_in[nh * size + x / a.dv * a.si + x % a.dv * a.sj] : 0.0f;
-    const float whole = (float)exp(ld * ops.seg_len);
+    const int used = max(1, (L + ops.seg_len - 1) / ops.seg_len);      // segments that hold frames; all but the last of them are whole
+    double S = a.s_in ? a.s_in[nh * size + x / a.dv * a.si + x % a.dv * a.sj] : 0.0;
+    const double whole = exp(ld * ops.seg_len);
     float* p = ops.seg_state[blockIdx.z] + nh * size + x;
-    for (int s = 0; s < ops.n_seg; ++s, p += heads * size) {
-        const int rows = min(L - s * ops.seg_len, ops.seg_len);
-        if (s > 0 && rows <= 0) return;
-        const float add = s + 1 < ops.n_seg && rows > 0 ? *p : 0.0f;
-        *p = S;
-        S = fmaf(S, rows == ops.seg_len ? whole : (float)exp(ld * rows), add);
+    for (int first = 0; first < used; first += U) {
+        float add[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) add[u] = p[min(first + u, ops.n_seg - 2) * heads * size];      // (behind the last: any)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (first + u < used) {
+                p[(first + u) * heads * size] = (float)S;
+                S = S * whole + add[u];
+            }
     }
 }
 
@@ -520,19 +577,22 @@ static void plan_segments(int T, int64_t works, int C, int& n_seg, int& seg_len)
     n_seg = std::max<int>(1, (int)((chunks + per - 1) / per));
 }
 namespace {
-struct ChunkShape { int DK, NT, C, slices; };
+struct ChunkShape { int DK, W, C, slices; };
 ChunkShape chunk_shape(int dtype, int dk, int dv) {
     ChunkShape s;
     s.DK = dk <= 64 ? 64 : dk <= 128 ? 128 : 256;
-    s.NT = dv <= 64 || s.DK == 256 ? 1 : 2;      // (256 rows x 32 columns a wavefront would not fit its registers)
-    s.C = dtype == DT_F32 || s.DK > 128 ? 32 : 64;
-    s.slices = (dv + 64 * s.NT - 1) / (64 * s.NT);
+    s.W = dv <= 64 ? 4 : 8;
+    s.C = chunk_frames(dtype == DT_F32, s.DK);
+    s.slices = (dv + 16 * s.W - 1) / (16 * s.W);
     return s;
 }
 }  // namespace
 
+// Few frames go one after another, and so do heads of less than 16 bytes, which the tiles of chunks cannot load.
+static bool by_frames(const AttnCall& c, const AttnOp& a) { return c.T <= ATTN_STEPS || std::min(a.dk, a.dv) * (c.dtype == DT_F32 ? 4 : 2) < 16; }
+
 int64_t attention_space(const AttnCall& c, const AttnOp* ops, int n_ops) {
-    if (c.T <= ATTN_STEPS || n_ops == 0) return 0;
+    if (n_ops == 0 || by_frames(c, ops[0])) return 0;
     int dk = 0, dv = 0;
     int64_t floats = 0;
     for (int i = 0; i < n_ops; ++i) { dk = std::max(dk, ops[i].dk); dv = std::max(dv, ops[i].dv); floats += ((int64_t)ops[i].dk * ops[i].dv * c.N * c.heads + 63) / 64 * 64; }
@@ -543,11 +603,19 @@ int64_t attention_space(const AttnCall& c, const AttnOp* ops, int n_ops) {
 }
 
 hipError_t launch_attention(const AttnCall& c, const AttnOp* ops, int n_ops, float* space, hipStream_t s) {
-    if (c.T <= ATTN_STEPS) return launch_attention_steps(c, ops, n_ops, s);
+    if (by_frames(c, ops[0])) return launch_attention_steps(c, ops, n_ops, s);
     ChunkOps co = {};
     int dk = 0, dv = 0;
-    bool state = false;
-    for (int i = 0; i < n_ops; ++i) { co.op[i] = ops[i]; dk = std::max(dk, ops[i].dk); dv = std::max(dv, ops[i].dv); state = state || ops[i].s_out; }
+    const int E = c.dtype == DT_F32 ? 4 : 8;      // units of 16 bytes
+    bool direct = true;
+    for (int i = 0; i < n_ops; ++i) {
+        const AttnOp& a = co.op[i] = ops[i];
+        dk = std::max(dk, a.dk); dv = std::max(dv, a.dv);
+        co.whole_state = co.whole_state || a.s_out;
+        direct = direct && a.dk % E == 0 && a.dv % E == 0;
+        for (const AttnTensor* x : {&a.q, &a.k, &a.v})
+            direct = direct && reinterpret_cast<uintptr_t>(x->p) % 16 == 0 && x->st % E == 0 && x->sn % E == 0 && x->sh % E == 0;
+    }
     const ChunkShape sh = chunk_shape(c.dtype, dk, dv);
     co.n_ops = n_ops; co.slices = sh.slices;
     plan_segments(c.T, (int64_t)c.N * c.heads * n_ops * sh.slices, sh.C, co.n_seg, co.seg_len);
@@ -558,27 +626,32 @@ hipError_t launch_attention(const AttnCall& c, const AttnOp* ops, int n_ops, flo
         }
     auto launch = [&](auto kernel, int segments) {
         co.works = (unsigned)((int64_t)segments * c.N * c.heads * n_ops * sh.slices);
-        kernel<<<(co.works + 7) / 8 * 8, 256, 0, s>>>(c, co);
+        kernel<<<(co.works + 7) / 8 * 8, 64 * sh.W, 0, s>>>(c, co);
         return hipGetLastError();
     };
-    auto go = [&](auto* t, auto DKc, auto NTc) {
+    auto start = [&](auto* t, auto DKc, auto Wc, auto directc) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        constexpr int DK = decltype(DKc)::value, NT = decltype(NTc)::value;
+        constexpr int DK = decltype(DKc)::value, W = decltype(Wc)::value;
+        constexpr bool DIRECT = decltype(directc)::value;
         if (co.n_seg > 1) {
-            hipError_t e = launch(attention_chunks_kernel<T, DK, NT, 3, true>, co.n_seg - 1);
+            hipError_t e = launch(attention_chunks_kernel<T, DK, W, DIRECT, true>, co.n_seg - 1);
             if (e != hipSuccess) return e;
-            attention_segments_kernel<<<dim3((unsigned)((dk * dv + 255) / 256), (unsigned)(c.N * c.heads), (unsigned)n_ops), 256, 0, s>>>(c, co);
+            auto* join = co.n_seg <= 4 ? attention_segments_kernel<4> : attention_segments_kernel<8>;
+            join<<<dim3((unsigned)((dk * dv + 255) / 256), (unsigned)(c.N * c.heads), (unsigned)n_ops), 256, 0, s>>>(c, co);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
-        if constexpr (sizeof(T) == 2) if (!state) return launch(attention_chunks_kernel<T, DK, NT, 2, false>, co.n_seg);
-        return launch(attention_chunks_kernel<T, DK, NT, 3, false>, co.n_seg);
+        return launch(attention_chunks_kernel<T, DK, W, DIRECT, false>, co.n_seg);
+    };
+    auto by_slice = [&](auto* t, auto DKc) {
+        const std::integral_constant<int, 4> four;
+        const std::integral_constant<int, 8> eight;
+        if (sh.W == 4) return direct ? start(t, DKc, four, std::true_type()) : start(t, DKc, four, std::false_type());
+        return direct ? start(t, DKc, eight, std::true_type()) : start(t, DKc, eight, std::false_type());
     };
     auto by_width = [&](auto* t) {
-        typedef std::integral_constant<int, 1> One;
-        typedef std::integral_constant<int, 2> Two;
-        if (sh.DK == 64) return sh.NT == 1 ? go(t, std::integral_constant<int, 64>(), One()) : go(t, std::integral_constant<int, 64>(), Two());
-        if (sh.DK == 128) return sh.NT == 1 ? go(t, std::integral_constant<int, 128>(), One()) : go(t, std::integral_constant<int, 128>(), Two());
-        return go(t, std::integral_constant<int, 256>(), One());
+        if (sh.DK == 64) return by_slice(t, std::integral_constant<int, 64>());
+        if (sh.DK == 128) return by_slice(t, std::integral_constant<int, 128>());
+        return by_slice(t, std::integral_constant<int, 256>());
     };
     return c.dtype == DT_F32 ? by_width((float*)nullptr) : by_width((bf16_t*)nullptr);
 }
