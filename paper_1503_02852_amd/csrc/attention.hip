@@ -20,48 +20,72 @@ __device__ __forceinline__ int length_of(const AttnCall& c, int n) { return c.le
 // ---------------------------------------------------------------------------------------------
 struct StepOps { AttnOp op[3]; };
 
-template <class T, int NR>
+// WIDE: rows of the state whose quads of columns are whole and aligned.
+template <class T, int NR, bool WIDE>
 __global__ void __launch_bounds__(256) attention_steps_kernel(AttnCall c, StepOps ops, int slices) {
     const AttnOp& a = ops.op[blockIdx.y];
     const int n = blockIdx.x / slices / c.heads, h = blockIdx.x / slices % c.heads;
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16, col = (blockIdx.x % slices) * 64 + tx * 4;
-    if ((blockIdx.x % slices) * 64 >= a.dv) return;      // (operators of one launch may differ in dv)
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16, col0 = (blockIdx.x % slices) * 64, col = col0 + tx * 4;
+    if (col0 >= a.dv) return;      // (operators of one launch may differ in dv)
     __shared__ float sum[2][4][64];
     const int L = length_of(c, n);
     const float g = expf(log_decay_of(c, h));
     const int64_t s0 = ((int64_t)n * c.heads + h) * a.dk * a.dv;
-    const bool wide = a.sj == 1 && a.dv % 4 == 0;        // (a row's quads are whole then, and aligned if the state is)
-    const bool aligned = wide && (((uintptr_t)a.s_in | (uintptr_t)a.s_out) & 15) == 0;
+    const int si = (int)a.si, sj = (int)a.sj;
     f32x4 S[NR];
+    // loads without conditions, all in flight together: places outside are read from the nearest inside and set to zero afterwards
+    if (a.s_in) {
+        const float* p = a.s_in + s0;
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        const int i = ty + 16 * r;
-        S[r] = 0.0f;
-        if (!a.s_in || i >= a.dk || col >= a.dv) continue;
-        const float* p = a.s_in + s0 + i * a.si + col * a.sj;
-        if (aligned) S[r] = *(const f32x4*)p;
-        else for (int j = 0; j < 4; ++j) if (col + j < a.dv) S[r][j] = p[j * a.sj];
-    }
+        for (int r = 0; r < NR; ++r) {
+            const int row = min(ty + 16 * r, a.dk - 1) * si;
+            if constexpr (WIDE) S[r] = *(const f32x4*)(p + row + min(col, a.dv - 4));
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j) S[r][j] = p[row + min(col + j, a.dv - 1) * sj];
+        }
+    } else
+#pragma unroll
+        for (int r = 0; r < NR; ++r) S[r] = 0.0f;
     const T* qp = (const T*)a.q.p + n * a.q.sn + (h / a.q.group) * a.q.sh;
     const T* kp = (const T*)a.k.p + n * a.k.sn + (h / a.k.group) * a.k.sh;
     const T* vp = (const T*)a.v.p + n * a.v.sn + (h / a.v.group) * a.v.sh;
-    for (int i = 0; i < L; ++i) {
-        const int t = a.reverse ? L - 1 - i : i;
-        float q[NR], k[NR];
+    T q[NR], k[NR], v[4];
+    auto load = [&](int t) {
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            const int row = ty + 16 * r;
-            q[r] = a.o.p && row < a.dk ? (float)qp[t * a.q.st + row] : 0.0f;
-            k[r] = row < a.dk ? (float)kp[t * a.k.st + row] * a.update : 0.0f;
+            const int row = min(ty + 16 * r, a.dk - 1);
+            if (a.o.p) q[r] = qp[t * a.q.st + row];
+            k[r] = kp[t * a.k.st + row];
         }
-        f32x4 v = 0.0f, o = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) if (col + j < a.dv) v[j] = (float)vp[t * a.v.st + col + j];
+        for (int j = 0; j < 4; ++j) v[j] = vp[t * a.v.st + min(col + j, a.dv - 1)];
+    };
+    if (L > 0) load(a.reverse ? L - 1 : 0);
+#pragma unroll
+    for (int r = 0; r < NR; ++r) asm volatile("" : "+v"(S[r]));
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) S[r][j] = ty + 16 * r < a.dk && col + j < a.dv ? S[r][j] : 0.0f;
+    for (int i = 0; i < L; ++i) {
+        const int t = a.reverse ? L - 1 - i : i;
+        float qf[NR], kf[NR];
+        f32x4 vf, o = 0.0f;
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            const bool there = ty + 16 * r < a.dk;
+            qf[r] = a.o.p && there ? (float)q[r] : 0.0f;
+            kf[r] = there ? (float)k[r] * a.update : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vf[j] = col + j < a.dv ? (float)v[j] : 0.0f;
+        if (i + 1 < L) load(a.reverse ? t - 1 : t + 1);
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
             if (a.early) S[r] *= g;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { S[r][j] = fmaf(k[r], v[j], S[r][j]); o[j] = fmaf(q[r], S[r][j], o[j]); }
+            for (int j = 0; j < 4; ++j) { S[r][j] = fmaf(kf[r], vf[j], S[r][j]); o[j] = fmaf(qf[r], S[r][j], o[j]); }
             if (!a.early) S[r] *= g;
         }
         if (!a.o.p) continue;
@@ -71,7 +95,7 @@ __global__ void __launch_bounds__(256) attention_steps_kernel(AttnCall c, StepOp
         float (*part)[64] = sum[i & 1];                  // (the next frame writes the other half: one barrier a frame)
         if (ty % 4 == 0) *(f32x4*)&part[ty / 4][tx * 4] = o;
         __syncthreads();
-        const int j = (blockIdx.x % slices) * 64 + threadIdx.x;
+        const int j = col0 + threadIdx.x;
         if (threadIdx.x < 64 && j < a.dv) {
             const float x = a.out * (part[0][threadIdx.x] + part[1][threadIdx.x] + part[2][threadIdx.x] + part[3][threadIdx.x]);
             const int64_t at = t * a.o.st + n * a.o.sn + h * a.o.sh + j;
@@ -80,13 +104,13 @@ __global__ void __launch_bounds__(256) attention_steps_kernel(AttnCall c, StepOp
         }
     }
     if (!a.s_out) return;
+    float* p = a.s_out + s0;
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
         const int i = ty + 16 * r;
         if (i >= a.dk || col >= a.dv) continue;
-        float* p = a.s_out + s0 + i * a.si + col * a.sj;
-        if (aligned) *(f32x4*)p = S[r];
-        else for (int j = 0; j < 4; ++j) if (col + j < a.dv) p[j * a.sj] = S[r][j];
+        if constexpr (WIDE) *(f32x4*)(p + i * si + col) = S[r];
+        else for (int j = 0; j < 4; ++j) if (col + j < a.dv) p[i * si + (col + j) * sj] = S[r][j];
     }
 }
 
@@ -554,15 +578,25 @@ __global__ void __launch_bounds__(256) attention_sum_heads_kernel(AttnCall c, co
 static hipError_t launch_attention_steps(const AttnCall& c, const AttnOp* ops, int n_ops, hipStream_t s) {
     StepOps so;
     int dk = 0, dv = 0;
-    for (int i = 0; i < n_ops; ++i) { so.op[i] = ops[i]; dk = std::max(dk, ops[i].dk); dv = std::max(dv, ops[i].dv); }
+    bool wide = true;
+    for (int i = 0; i < n_ops; ++i) {
+        const AttnOp& a = so.op[i] = ops[i];
+        dk = std::max(dk, a.dk); dv = std::max(dv, a.dv);
+        wide = wide && a.sj == 1 && a.dv % 4 == 0 && ((reinterpret_cast<uintptr_t>(a.s_in) | reinterpret_cast<uintptr_t>(a.s_out)) & 15) == 0;
+    }
     const int slices = (dv + 63) / 64;
     const dim3 grid((unsigned)c.N * c.heads * slices, (unsigned)n_ops);
-    auto go = [&](auto* t) {
+    auto start = [&](auto* t, auto rows) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        if (dk <= 64) attention_steps_kernel<T, 4><<<grid, 256, 0, s>>>(c, so, slices);
-        else if (dk <= 128) attention_steps_kernel<T, 8><<<grid, 256, 0, s>>>(c, so, slices);
-        else attention_steps_kernel<T, 16><<<grid, 256, 0, s>>>(c, so, slices);
+        constexpr int NR = decltype(rows)::value;
+        auto* kernel = wide ? attention_steps_kernel<T, NR, true> : attention_steps_kernel<T, NR, false>;
+        kernel<<<grid, 256, 0, s>>>(c, so, slices);
         return hipGetLastError();
+    };
+    auto go = [&](auto* t) {
+        if (dk <= 64) return start(t, std::integral_constant<int, 4>());
+        if (dk <= 128) return start(t, std::integral_constant<int, 8>());
+        return start(t, std::integral_constant<int, 16>());
     };
     return c.dtype == DT_F32 ? go((float*)nullptr) : go((bf16_t*)nullptr);
 }

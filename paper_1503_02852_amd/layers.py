@@ -52,7 +52,7 @@ def _dtype(dtype, allowed=DTYPES):
 
 
 def _tensor(name, x, shape, dtype, device):
-    if x.dtype != dtype or tuple(x.shape) != shape or x.device != device:
+    if x.dtype is not dtype or x.shape != shape or x.device != device:
         raise _invalid(f"{name}: expected {dtype} {list(shape)} on {device}, got {x.dtype} {list(x.shape)} on {x.device}")
     return x
 
@@ -91,11 +91,10 @@ class LinearAttention:
     def _frames(self, name, x, like):
         if x is None:
             return None
-        _tensor(name, x, self.shapes[like], self.dtype, self.dev)
-        st, sn, sh, one = x.stride()
+        st, sn, sh, one = _tensor(name, x, self.shapes[like], self.dtype, self.dev).stride()
         if one != 1 and x.shape[3] > 1:
             raise _invalid(f"{name}: a head's units must lie next to each other")
-        return C.byref(Frames(x.data_ptr(), st, sn, sh))
+        return Frames(x.data_ptr(), st, sn, sh)      # (ctypes passes its address)
 
     def _common(self, log_decay, lengths):
         return (_flat("log_decay", log_decay, (self.heads,), torch.float32, self.dev), _flat("lengths", lengths, (self.N,), torch.int32, self.dev))
@@ -130,7 +129,7 @@ def _rows(name, x, rows, dim, dtype, device):
     """(address, elements from a row to the next) of a tensor of `rows` evenly spaced rows; (None, 0) for None."""
     if x is None:
         return None, 0
-    if x.dtype != dtype or x.device != device or x.dim() < 1 or x.shape[-1] != dim or x.numel() != rows * dim:
+    if x.dtype is not dtype or x.device != device or x.dim() < 1 or x.shape[-1] != dim or x.numel() != rows * dim:
         raise _invalid(f"{name}: expected {dtype}, {rows} rows of {dim} on {device}, got {x.dtype} {list(x.shape)} on {x.device}")
     if x.is_contiguous():
         return x.data_ptr(), dim
