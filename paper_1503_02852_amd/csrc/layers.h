@@ -68,7 +68,10 @@ struct AttnOp {
 };
 struct AttnCall { int T, N, heads, dtype; const float* log_decay; const int32_t* lengths; };
 constexpr int ATTN_MAX_DIM = 256;
-constexpr int ATTN_STEPS = 16;      // windows of at most so many frames go frame by frame, longer ones in chunks
+// Windows of at most so many frames go frame by frame, longer ones in chunks.  Frame by frame / in chunks, us for T = 2, 4, 8 (in a graph):
+// 64 streams x 16 heads x 128 x 128, bf16: 29 / 33, 37 / 34, 52 / 34;  64 x 64, bf16: 9.5 / 13.8, 12.4 / 13.9, 18.4 / 13.9;
+// 64 x 8 heads x 128 x 128, fp32: 20 / 32, 26 / 31, 38 / 31;  one stream, 16 heads x 128 x 128, bf16: 6.6 / 9.6, 9.7 / 9.6, 15.9 / 9.6.
+constexpr int ATTN_STEPS = 4;
 // Up to three operators side by side.  space: attention_space bytes.
 int64_t attention_space(const AttnCall& c, const AttnOp* ops, int n_ops);
 hipError_t launch_attention(const AttnCall& c, const AttnOp* ops, int n_ops, float* space, hipStream_t s);

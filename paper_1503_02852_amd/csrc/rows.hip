@@ -247,18 +247,29 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) add_norm_grad_kernel(Ad
     for (int v = 0; v < NV; ++v) store8<WHOLE>(out + (v * TPR + lane) * 8, dg[v], dim - (v * TPR + lane) * 8);
 }
 
-// out[c] = sum of `rows` rows of `partial`, in one order: 16 runs of rows for each of 64 columns, then the runs.
+// out[c] = sum of `rows` rows of `partial`, in one order: 32 runs of rows for each of 32 columns, a run in eight sums (eight loads in
+// flight), then the runs.
 __global__ void __launch_bounds__(1024) sum_rows_kernel(const float* partial, float* out, int rows, int dim) {
-    __shared__ float part[16][64];
-    const int c = blockIdx.x * 64 + threadIdx.x % 64, run = threadIdx.x / 64;
-    float s = 0.0f;
-    if (c < dim)
-        for (int r = run; r < rows; r += 16) s += partial[(int64_t)r * dim + c];
-    part[run][threadIdx.x % 64] = s;
+    __shared__ float part[32][33];
+    const int x = threadIdx.x % 32, c = blockIdx.x * 32 + x, run = threadIdx.x / 32;
+    const float* p = partial + min(c, dim - 1);
+    float s[8] = {};
+    int r = run;
+    for (; r + 7 * 32 < rows; r += 8 * 32) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p[(int64_t)(r + 32 * i) * dim];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += v[i];
+    }
+    for (; r < rows; r += 32) s[0] += p[(int64_t)r * dim];
+    part[run][x] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
     __syncthreads();
     if (run > 0 || c >= dim) return;
-    for (int i = 1; i < 16; ++i) s += part[i][threadIdx.x];
-    out[c] = s;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) sum += part[i][x];
+    out[c] = sum;
 }
 
 __global__ void __launch_bounds__(256) zero_kernel(float* p, int n) {
@@ -353,7 +364,7 @@ hipError_t launch_add_norm_grad(int dtype, const AddNormGradArgs& a, hipStream_t
         });
     });
     if (e == hipSuccess && a.dgain && a.blocks > 1) {
-        sum_rows_kernel<<<(a.dim + 63) / 64, 1024, 0, s>>>(a.partial, a.dgain, a.blocks, a.dim);
+        sum_rows_kernel<<<(a.dim + 31) / 32, 1024, 0, s>>>(a.partial, a.dgain, a.blocks, a.dim);
         e = hipGetLastError();
     }
     return e;
