@@ -55,8 +55,22 @@ enum rnn_status {
  * outputs, then an activation function) and multiplicative layers (element-wise product), and
  * allows other aggregation functions; RNN_NODE_MAX takes the element-wise maximum of the incoming
  * connection outputs (its error terms go to the connection that holds the maximum, to the one
- * with the lowest edge index if several do). */
-enum { RNN_NODE_INPUT = 0, RNN_NODE_ADD = 1, RNN_NODE_MUL = 2, RNN_NODE_MAX = 3 };
+ * with the lowest edge index if several do).
+ * Three kinds work on whole frames: their output units depend on more than the same unit of the
+ * connections, so they may not be part of a recurrent node, and have no activation function.  They
+ * are computed for all frames of a window at once.  s: the sum of the incoming connection outputs.
+ *   RNN_NODE_NORM       y = gain * s / sqrt(mean(s^2) + RNN_NORM_EPS) over the node's units (at most
+ *                       16384); the gain is the node's bias vector if has_bias, else 1.  Two
+ *                       connections make it the norm of a residual sum.
+ *   RNN_NODE_ATTENTION  linear attention with a decay per head.  Three incoming connections, in edge
+ *                       order: queries, keys, values; each head of stream n keeps a state
+ *                       S(t) = exp(log_decay) S(t - 1) + k(t) v(t)^T, and y(t) = scale S(t)^T q(t).
+ *                       rnn_set_attention gives heads, scale and decays.  A fresh window starts from
+ *                       S = 0, one moved ahead from the state that the earlier frames left.
+ *   RNN_NODE_DROPOUT    y = s / (1 - p) or 0 (rnn_set_dropout; before it, y = s).
+ * rnngraph_layers.h has the same three for the caller's own tensors, in more types. */
+enum { RNN_NODE_INPUT = 0, RNN_NODE_ADD = 1, RNN_NODE_MUL = 2, RNN_NODE_MAX = 3, RNN_NODE_NORM = 4, RNN_NODE_ATTENTION = 5, RNN_NODE_DROPOUT = 6 };
+#define RNN_NORM_EPS 1e-6f
 /* Activation functions f_k (Section 2.1 leaves them open); softmax is allowed on output nodes
  * only and is paired with the cross-entropy criterion, the case for which Section 2.2 writes the
  * output delta out.  RNN_ACT_RELU is the rectifier max(0, s); its derivative at s = 0 counts as 0. */
@@ -84,7 +98,9 @@ typedef struct { int32_t src, dst, delay, wkind; } rnn_edge_desc;
  * input node; a non-input node has no incoming edge; an input node has a bias, an activation or
  * is an output; softmax on a node that is not a cross-entropy output, a cross-entropy output
  * that is not additive-softmax, a squared-error output that is not additive or has softmax;
- * an output node with outgoing edges; has_bias on a multiplicative or maximum node; there is no output
+ * an output node with outgoing edges; has_bias on a multiplicative, maximum, attention or dropout node;
+ * a norm, attention or dropout node with an activation or inside a recurrent component; a norm node of
+ * more than 16384 units; an attention node without exactly three incoming edges; there is no output
  * node; or the delay-0 edges contain a cycle (Section 3.1 needs the per-step remainder to be a
  * DAG). */
 int rnn_graph_create(const rnn_node_desc* nodes, int32_t n_nodes,
@@ -145,7 +161,8 @@ int rnn_forward(rnn_graph* g, const float* d_weights, const float* const* d_inpu
  * the same T and N (RNN_ERR_SEQUENCE otherwise): delayed connections read them as y(t - d), so a
  * window computed in pieces equals the window computed at once (to the last bit, but where products of
  * 1,024 columns and more over few rows are shared by several workgroups, whose parts are added in any
- * order; rnn_set_deterministic keeps to one).  Arguments as in rnn_forward,
+ * order; rnn_set_deterministic keeps to one; and but for attention nodes, whose sums are grouped by chunks
+ * counted from the piece's first frame: equal within fp32 rounding).  Arguments as in rnn_forward,
  * which is rnn_forward_range(.., 0, T, ..).  A call with t_begin = 0 starts a fresh window: zero
  * state in front of it, control words cleared.  rnn_bptt needs the whole window computed. */
 int rnn_forward_range(rnn_graph* g, const float* d_weights, const float* const* d_inputs,
@@ -161,6 +178,21 @@ int rnn_forward_range(rnn_graph* g, const float* d_weights, const float* const* 
  * the node may only have full out-connections.  d_inputs[input] of rnn_forward is then ignored
  * (may be NULL) and rnn_output of the node yields NULL.  d_indices = NULL returns to dense input. */
 int rnn_set_onehot_input(rnn_graph* g, int32_t input, const int32_t* d_indices);
+
+/* Heads of an attention node (they divide its units into heads of at most 256), the factor of its
+ * outputs, and d_log_decay, DEVICE float [heads], each at most 0 (0: nothing is forgotten, -inf:
+ * everything; positive values count as 0), which must stay valid and unchanged while windows run; it
+ * has no gradient.  Needed before rnn_workspace_bytes and the first window (RNN_ERR_SEQUENCE); ends the
+ * current window. */
+int rnn_set_attention(rnn_graph* g, int32_t node, int32_t heads, float scale, const float* d_log_decay);
+
+/* Dropout of a node: a unit of a frame is dropped with probability p (in steps of 1 / 65536), kept ones
+ * are divided by 1 - p.  Which ones is a function of seed, offset + *d_offset (DEVICE, read when the
+ * kernels run, must not change from rnn_forward to rnn_bptt; NULL: 0), the stream and the frame, counted
+ * from the last fresh window's first on through rnn_shift_window: rnn_dropout (rnngraph_layers.h) of
+ * row frame * N + stream.  Nothing is stored, rnn_bptt takes the same ones.  A fresh window draws the same ones
+ * again unless seed or offset differ.  p = 0 for inference.  Ends the current window. */
+int rnn_set_dropout(rnn_graph* g, int32_t node, float p, uint64_t seed, uint64_t offset, const uint64_t* d_offset);
 
 /* Moves the window `frames` frames ahead in time (Section 3.2): every node's activations of
  * frame t + frames become those of frame t, for t < T - frames; the last `frames` frames are then
@@ -192,7 +224,7 @@ int rnn_output(const rnn_graph* g, int32_t node, const float** d_y);
 int rnn_bptt(rnn_graph* g, const float* d_weights, const void* const* d_targets, void* hip_stream);
 
 /* DEVICE view of dE_total/ds_k [T][N][dim] (the paper's -delta_k) after rnn_bptt; not defined
- * for input nodes. */
+ * for input nodes.  For an attention node, which has three sums: dE_total/dy_k. */
 int rnn_state_grad(const rnn_graph* g, int32_t node, const float** d_ds);
 
 /* Weight gradients (last equation of Section 2.2, summed over the N streams as in Section 3.2).

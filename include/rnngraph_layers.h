@@ -3,7 +3,7 @@
  * attention with a decay for each head (a recurrent layer whose state is a matrix), the residual
  * sum with dropout and root-mean-square norm, and dropout.  Networks have the same layers as node
  * kinds (RNN_NODE_ATTENTION, RNN_NODE_NORM, RNN_NODE_DROPOUT of rnngraph.h, in fp32); the functions
- * here take other types and strides too, and need no graph.
+ * here take other types, strides and lengths too, and need no graph.
  *
  * Conventions
  *  - As in rnngraph.h: 0 or a negative rnn_status, rnn_last_error() for the message, "d_" pointers
@@ -17,7 +17,10 @@
  *    data[t * stride_t + n * stride_n + h * stride_h + i], strides in elements, of any sign and size.
  *    Inputs may overlap each other; an output may overlap nothing, and two of its elements may
  *    not share a place.  Alignment: that of the element type.
- *  - Arithmetic is fp32 whatever the type of the tensors; what is stored is rounded once, to nearest.
+ *  - Sums, statistics and states are fp32 whatever the type of the tensors, and what is stored is rounded once, to
+ *    nearest.  Attention on RNN_BF16 tensors multiplies with the matrix instructions for bf16: the scores between frames of
+ *    a chunk and, for outputs and gradients, the state that the chunk starts from are rounded to bf16 as their
+ *    operands (the state that is handed on is not).
  */
 #ifndef RNNGRAPH_LAYERS_H
 #define RNNGRAPH_LAYERS_H
@@ -35,7 +38,9 @@ enum rnn_dtype { RNN_F32 = 0, RNN_BF16 = 1, RNN_F16 = 2 };
  *     S(t) = exp(log_decay[h]) S(t - 1) + k(t) v(t)^T          o(t) = scale S(t)^T q(t)
  * that is o(t) = scale sum_{s <= t} exp((t - s) log_decay[h]) (q(t) . k(s)) v(s) + the part of
  * the state before the window.  Frames are worked on together, in chunks (Section 3.1's aim for
- * a recurrence that has no nonlinearity); few frames (rnn_linear_attention_steps) one after another.
+ * a recurrence that has no nonlinearity); few frames (up to 4) one after another.  An infinity or NaN in a
+ * frame makes outputs of earlier frames of its chunk (up to 63 back) NaN as well as later ones; other
+ * streams and heads never.
  *   T, N        frames and streams; T = 0 and N = 0 are allowed
  *   heads       heads of q and o; kv_heads heads of k and v, heads = kv_heads * group: head h reads
  *               key / value head h / group

@@ -27,6 +27,9 @@ Readings where the paper is silent (all listed in the design notes of the reposi
     epsilon are propagated only while t > t0', but the connection outputs z_n(t) and the
     weight-gradient terms eps_m(t) y_k(t - d_m)^T of the frames t > t0' use the real
     y_k(t - d_m), also where t - d_m <= t0'; error terms from frames after the window are zero;
+  * three kinds of layers that work on whole frames, for which the paper leaves room as it does for
+    the maximum: norm (4), linear attention (5) and dropout (6), as include/rnngraph.h defines them
+    (layers_oracle.py has the dropout generator);
   * E_total = sum over frames, streams and output nodes of E(t) (no averaging).  Two error
     criteria (Section 2.2: the initial delta of an output layer depends on the criterion E(t) and
     on the layer's activation function): is_output = 1, softmax with minimum
@@ -49,7 +52,10 @@ from __future__ import annotations
 
 import numpy as np
 
-INPUT, ADD, MUL, MAX = 0, 1, 2, 3
+from oracle import layers_oracle
+
+INPUT, ADD, MUL, MAX, NORM, ATTENTION, DROPOUT = 0, 1, 2, 3, 4, 5, 6
+NORM_EPS = 1e-6
 CROSS_ENTROPY, SQUARED_ERROR = 1, 2          # values of a node's is_output
 LINEAR, SIGMOID, TANH, SOFTMAX, RELU = 0, 1, 2, 3, 4
 FULL, DIAG, IDENTITY = 0, 1, 2
@@ -127,6 +133,23 @@ def _activation_derivative(act, y):
     raise ValueError(act)
 
 
+def _dropout_factor(n, t, N):
+    """[N, dim] of frame t: 1 / (1 - p) or 0."""
+    return layers_oracle.dropout_factor(N, n["dim"], *n.get("dropout", (0.0, 0, 0)), first_row=t * N)
+
+
+def _heads(n, x):
+    return x.reshape(x.shape[0], n["heads"], -1)
+
+
+def _decay(n):
+    return np.exp(np.minimum(np.asarray(n["log_decay"], dtype=np.float64), 0.0))[:, None, None]
+
+
+def _outer(a, b):
+    return a[..., :, None] * b[..., None, :]
+
+
 def forward(nodes, edges, weights, biases, inputs, T, N, history=None):
     """Forward pass over frames 1..T (stored at index 0..T-1).
 
@@ -149,6 +172,9 @@ def forward(nodes, edges, weights, biases, inputs, T, N, history=None):
     for k, n in enumerate(nodes):
         if n["kind"] == INPUT:
             y[k][:] = np.asarray(inputs[k], dtype=np.float64)
+    state = {}       # attention nodes: S [N, heads, d, d] after the last frame
+    assert history is None or all(n["kind"] != ATTENTION for n in nodes)
+
     def source_activation(k, tau):
         """y_k(tau); tau < 0 lies before the window: the carried history, else zero."""
         if tau >= 0:
@@ -178,6 +204,17 @@ def forward(nodes, edges, weights, biases, inputs, T, N, history=None):
                 s = z[anterior[k][0]][t]
                 for m in anterior[k][1:]:
                     s = np.maximum(s, z[m][t])
+            elif n["kind"] in (NORM, DROPOUT):
+                s = sum(z[m][t] for m in anterior[k])
+                if n["kind"] == NORM:
+                    s = s / np.sqrt((s * s).mean(axis=1, keepdims=True) + NORM_EPS)
+                    s = s if B[k] is None else s * B[k]
+                else:
+                    s = s * _dropout_factor(n, t, N)
+            elif n["kind"] == ATTENTION:
+                q, kk, v = (_heads(n, z[m][t]) for m in anterior[k])
+                state[k] = _decay(n) * state.get(k, 0.0) + _outer(kk, v)
+                s = n["scale"] * (q[..., None] * state[k]).sum(axis=2).reshape(N, -1)
             else:
                 s = np.ones((N, n["dim"]))
                 for m in anterior[k]:
@@ -230,6 +267,15 @@ def bptt(nodes, edges, weights, biases, y, z, targets, T, N, t_first=0):
     delta = [np.zeros((T, N, n["dim"])) for n in nodes]
     grad_w = [None if w is None else np.zeros_like(w) for w in W]
     grad_b = [None if b is None else np.zeros(nodes[k]["dim"]) for k, b in enumerate(biases)]
+    states, dstate = {}, {}      # attention nodes: S after every frame; -dE/dS of the state after the frame
+    for k, n in enumerate(nodes):
+        if n["kind"] == ATTENTION:
+            S = np.zeros((N, n["heads"], n["dim"] // n["heads"], n["dim"] // n["heads"]))
+            states[k], dstate[k] = [], np.zeros_like(S)
+            for t in range(T):
+                _, kk, v = (_heads(n, z[m][t]) for m in anterior[k])
+                S = _decay(n) * S + _outer(kk, v)
+                states[k].append(S)
     for t in range(T - 1, t_first - 1, -1):
         for k in reversed(order):
             n = nodes[k]
@@ -250,12 +296,32 @@ def bptt(nodes, edges, weights, biases, y, z, targets, T, N, t_first=0):
                 delta[k][t] = d
             else:
                 delta[k][t] = acc[k][t] * _activation_derivative(n["act"], y[k][t])
-            if grad_b[k] is not None:
+            if n["kind"] == NORM:      # delta so far: -dE/dy
+                s = sum(z[m][t] for m in anterior[k])
+                r = 1.0 / np.sqrt((s * s).mean(axis=1, keepdims=True) + NORM_EPS)
+                dy = delta[k][t]
+                if grad_b[k] is not None:
+                    grad_b[k] -= (dy * s * r).sum(axis=0)
+                    dy = dy * np.asarray(biases[k], dtype=np.float64)
+                delta[k][t] = r * (dy - s * r * (dy * s * r).mean(axis=1, keepdims=True))
+            elif n["kind"] == DROPOUT:
+                delta[k][t] = delta[k][t] * _dropout_factor(n, t, N)
+            elif n["kind"] == ATTENTION:      # (delta stays -dE/dy)
+                q, kk, v = (_heads(n, z[m][t]) for m in anterior[k])
+                do = n["scale"] * _heads(n, delta[k][t])
+                dstate[k] = dstate[k] + _outer(q, do)
+                parts = [(states[k][t] * do[:, :, None, :]).sum(axis=3), (dstate[k] * v[:, :, None, :]).sum(axis=3),
+                         (dstate[k] * kk[..., None]).sum(axis=2)]
+                parts = [x.reshape(N, -1) for x in parts]
+                dstate[k] = dstate[k] * _decay(n)
+            if grad_b[k] is not None and n["kind"] != NORM:
                 grad_b[k] -= delta[k][t].sum(axis=0)
             for m in anterior[k]:
                 e = edges[m]
-                if n["kind"] == ADD:
+                if n["kind"] in (ADD, NORM, DROPOUT):
                     eps = delta[k][t]
+                elif n["kind"] == ATTENTION:
+                    eps = parts[anterior[k].index(m)]
                 elif n["kind"] == MAX:
                     # ds/dz_m is 1 where connection m holds the maximum (the first one, if several do), else 0
                     eps = delta[k][t].copy()

@@ -16,7 +16,7 @@ EXPORTS = ["rnn_graph_create", "rnn_graph_destroy", "rnn_graph_schedule", "rnn_p
            "rnn_edge_param_offset", "rnn_bias_param_offset", "rnn_workspace_bytes", "rnn_forward",
            "rnn_forward_range", "rnn_shift_window", "rnn_set_onehot_input",
            "rnn_output", "rnn_bptt", "rnn_state_grad", "rnn_grads", "rnn_check", "rnn_set_deterministic", "rnn_specialise",
-           "rnn_forward_static", "rnn_last_error"]
+           "rnn_forward_static", "rnn_last_error", "rnn_set_attention", "rnn_set_dropout"]
 # measurement and inspection aids (include/rnngraph_aux.h)
 AUX_EXPORTS = ["rnn_step_build", "rnn_debug_read_control", "rnn_profile_enable", "rnn_profile_read", "rnn_plan_work"]
 # layers on the caller's own tensors (include/rnngraph_layers.h)
@@ -85,6 +85,10 @@ def load_library(build_if_missing=True):
     lib.rnn_forward_static.restype = C.c_int
     lib.rnn_set_onehot_input.argtypes = [vp, C.c_int32, vp]
     lib.rnn_set_onehot_input.restype = C.c_int
+    lib.rnn_set_attention.argtypes = [vp, C.c_int32, C.c_int32, C.c_float, vp]
+    lib.rnn_set_attention.restype = C.c_int
+    lib.rnn_set_dropout.argtypes = [vp, C.c_int32, C.c_float, C.c_uint64, C.c_uint64, vp]
+    lib.rnn_set_dropout.restype = C.c_int
     lib.rnn_shift_window.argtypes = [vp, C.c_int32, vp]
     lib.rnn_shift_window.restype = C.c_int
     lib.rnn_output.argtypes = [vp, C.c_int32, C.POINTER(vp)]
@@ -242,6 +246,12 @@ class Graph:
 
     def set_onehot_input(self, input_index, d_indices):
         _check(self.lib.rnn_set_onehot_input(self.handle, input_index, d_indices))
+
+    def set_attention(self, node, heads, d_log_decay, scale=1.0):
+        _check(self.lib.rnn_set_attention(self.handle, node, heads, scale, d_log_decay))
+
+    def set_dropout(self, node, p, seed, offset=0, d_offset=None):
+        _check(self.lib.rnn_set_dropout(self.handle, node, p, seed, offset, d_offset))
 
     def shift_window(self, frames, stream=0):
         _check(self.lib.rnn_shift_window(self.handle, frames, stream))

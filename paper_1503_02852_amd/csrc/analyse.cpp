@@ -21,11 +21,16 @@ std::string validate_graph(const std::vector<GNode>& nodes, const std::vector<GE
     int n_outputs = 0;
     for (int k = 0; k < K; ++k) {
         const GNode& n = nodes[k];
-        if (n.kind < NODE_INPUT || n.kind > NODE_MAX) { e << "node " << k << ": unknown kind " << n.kind; return e.str(); }
+        if (n.kind < NODE_INPUT || n.kind > NODE_DROPOUT) { e << "node " << k << ": unknown kind " << n.kind; return e.str(); }
         if (n.act < ACT_LINEAR || n.act > ACT_RELU) { e << "node " << k << ": unknown activation " << n.act; return e.str(); }
         if (n.dim <= 0) { e << "node " << k << ": dim must be positive"; return e.str(); }
         if (n.kind == NODE_INPUT && (n.has_bias || n.is_output || n.act != ACT_LINEAR)) {
             e << "node " << k << ": an input node has no bias, no activation and is not an output"; return e.str();
+        }
+        if (whole_frames(n.kind)) {
+            if (n.act != ACT_LINEAR) { e << "node " << k << ": a norm, attention or dropout node has no activation"; return e.str(); }
+            if (n.kind != NODE_NORM && n.has_bias) { e << "node " << k << ": an attention or dropout node has no bias"; return e.str(); }
+            if (n.kind == NODE_NORM && n.dim > 16384) { e << "node " << k << ": a norm node has at most 16384 units"; return e.str(); }
         }
         if ((n.kind == NODE_MUL || n.kind == NODE_MAX) && n.has_bias) { e << "node " << k << ": a multiplicative or maximum node has no bias"; return e.str(); }
         if (n.is_output < OUT_NONE || n.is_output > OUT_SQUARED_ERROR) { e << "node " << k << ": unknown output kind " << n.is_output; return e.str(); }
@@ -56,6 +61,8 @@ std::string validate_graph(const std::vector<GNode>& nodes, const std::vector<GE
         if (nodes[ed.src].is_output) { e << "edge " << m << ": leaves an output node"; return e.str(); }
         ++n_in[ed.dst]; ++n_out[ed.src];
     }
+    for (int k = 0; k < K; ++k)
+        if (nodes[k].kind == NODE_ATTENTION && n_in[k] != 3) { e << "node " << k << ": an attention node has three incoming edges (queries, keys, values)"; return e.str(); }
     for (int k = 0; k < K; ++k)
         if (nodes[k].kind != NODE_INPUT && n_in[k] == 0) { e << "node " << k << ": non-input node without incoming edge"; return e.str(); }
     return "";

@@ -4,6 +4,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <algorithm>
+#include <cmath>
 #include <array>
 #include <tuple>
 #include <cstring>
@@ -15,6 +16,7 @@
 
 #include "../../include/rnngraph.h"
 #include "../../include/rnngraph_aux.h"
+#include "../../include/rnngraph_layers.h"
 #include "jit.h"
 #include "kernels.h"
 #include "layers.h"
@@ -41,6 +43,10 @@ struct Layout {
     int64_t partial_off = -1;             // partial sums of the two-dimensional matrix-core kernels (one launch at a time)
     std::vector<int64_t> idx_off;         // per exec node id: int32 [(hist + T)][N] copy of a one-hot input's class indices, or -1
     int64_t wt_off = -1;                  // transposed copies of the matrices the streaming kernels read transposed (parameter layout)
+    // norm, attention and dropout layers: per layer, the states of an attention layer at the window's start and behind the frames computed so
+    // far; scratch that each of their launches may use; int64 frames x streams that lie before the window (for dropout's numbers)
+    std::vector<int64_t> state_off, reached_off;
+    int64_t scratch_off = -1, passed_off = -1;
     int64_t frames_off = 0;               // per buffer id: int64 floats per frame of a frame tensor of the workspace (has history frames), else 0
     int64_t total = 0;
     int64_t uncounted_bytes = 0;          // of total, what the static workspace's limit leaves out: twins that only windows of no whole
@@ -55,7 +61,9 @@ int64_t g_layout_skew = 4352;      // bytes, a multiple of 256 (RNNG_LAYOUT_SKEW
 // transposed_copy: a streaming kernel of the window reads matrices transposed
 // twins: per buffer id, whether a step launch of the window polls this twin
 // layouts: most layouts of step launches that the window's plan tables carry
-Layout make_layout(const Plan& P, int T, int N, int64_t partial_floats, bool transposed_copy, const std::vector<char>& twins, int layouts) {
+// state_bytes, scratch_bytes: of the layers (Layout::state_off, scratch_off)
+Layout make_layout(const Plan& P, int T, int N, int64_t partial_floats, bool transposed_copy, const std::vector<char>& twins, int layouts,
+                   const std::vector<int64_t>& state_bytes, int64_t scratch_bytes) {
     Layout L;
     int n_alloc = 0;
     const int K = (int)P.xnodes.size();
@@ -89,6 +97,14 @@ Layout make_layout(const Plan& P, int T, int N, int64_t partial_floats, bool tra
     L.idx_off.assign(P.xnodes.size(), -1);
     for (size_t k = 0; k < P.xnodes.size(); ++k)
         if (P.xnodes[k].kind == NODE_INPUT && P.input_delayed[k]) { L.idx_off[k] = cur; cur = align_up(cur + F * 4, 256); }
+    if (!P.layers.empty()) { L.passed_off = cur; cur += 256; }
+    L.state_off.assign(P.layers.size(), -1); L.reached_off = L.state_off;
+    for (size_t i = 0; i < P.layers.size(); ++i)
+        if (state_bytes[i] > 0) {
+            L.state_off[i] = cur; cur = align_up(cur + state_bytes[i], 256);
+            L.reached_off[i] = cur; cur = align_up(cur + state_bytes[i], 256);
+        }
+    if (scratch_bytes > 0) { L.scratch_off = cur; cur = align_up(cur + scratch_bytes, 256); }
     // tile-blocked twins, behind everything else
     for (int b = 0; b < P.n_bufs; ++b)
         if (twins[b]) {
@@ -381,6 +397,40 @@ struct rnn_graph {
     // the workspace layout of a window of T frames and N streams (kept for the last shape asked for)
     Layout cached_layout;
     int cached_T = 0, cached_N = 0;
+    // What rnn_set_attention and rnn_set_dropout gave, per Plan::layers; frames of the window that the attention layers' running states cover (-1: unknown).
+    struct LayerSetting { int heads = 0; float scale = 1.0f; const float* d_log_decay = nullptr; float p = 0.0f; uint64_t seed = 0, offset = 0; const uint64_t* d_offset = nullptr; };
+    std::vector<LayerSetting> layer_settings;
+    int attention_upto = -1;
+    rnn_linear_attention_desc attention_desc(int i, int T, int N) const {
+        const LayerSetting& ls = layer_settings[i];
+        const int dim = plan.xnodes[plan.layers[i].node].dim;
+        return rnn_linear_attention_desc{T, N, ls.heads, ls.heads, dim / ls.heads, dim / ls.heads, RNN_F32, ls.scale};
+    }
+    // RNN_OK, or why a window of T frames and N streams cannot run
+    int check_layers(int T, int N) const {
+        for (size_t i = 0; i < plan.layers.size(); ++i) {
+            if (plan.layers[i].kind != NODE_ATTENTION) continue;
+            if (layer_settings[i].heads == 0) return fail(RNN_ERR_SEQUENCE, "node " + std::to_string(plan.layers[i].node) + ": an attention node needs rnn_set_attention");
+            const rnn_linear_attention_desc d = attention_desc((int)i, T, N);
+            const int64_t b = rnn_linear_attention_workspace_bytes(&d, 1);
+            if (b < 0) return (int)b;
+        }
+        return RNN_OK;
+    }
+    // bytes of each attention layer's state; returns those of the scratch that any launch of the layers needs (check_layers has passed)
+    int64_t layer_space(int T, int N, std::vector<int64_t>& state_bytes) const {
+        int64_t scratch = 0;
+        for (size_t i = 0; i < plan.layers.size(); ++i) {
+            const int dim = plan.xnodes[plan.layers[i].node].dim;
+            if (plan.layers[i].kind == NODE_NORM && plan.xnodes[plan.layers[i].node].has_bias)
+                scratch = std::max<int64_t>(scratch, (int64_t)norm_grad_blocks((int64_t)T * N, dim) * dim * 4);
+            if (plan.layers[i].kind != NODE_ATTENTION) continue;
+            const rnn_linear_attention_desc d = attention_desc((int)i, T, N);
+            state_bytes[i] = (int64_t)N * dim * d.dim_v * 4;
+            for (int backward = 0; backward < 2; ++backward) scratch = std::max(scratch, rnn_linear_attention_workspace_bytes(&d, backward));
+        }
+        return scratch;
+    }
     const Layout& layout_for(int T, int N) {
         if (cached_T != T || cached_N != N) {
             const int64_t partial = partial_frame_floats(N);
@@ -389,7 +439,9 @@ struct rnn_graph {
             int layouts = 0;
             for (const bool sizes_ok : {true, false})      // (whether the chain launches can run is known with the layout only)
                 layouts = std::max(layouts, (int)(step_layouts(N, sizes_ok).words.size() / STEP_LAYOUT_WORDS));
-            cached_layout = make_layout(plan, T, N, partial, copy, twins, layouts);
+            std::vector<int64_t> state_bytes(plan.layers.size(), 0);
+            const int64_t scratch_bytes = layer_space(T, N, state_bytes);
+            cached_layout = make_layout(plan, T, N, partial, copy, twins, layouts, state_bytes, scratch_bytes);
             cached_T = T; cached_N = N;
         }
         return cached_layout;
@@ -1183,6 +1235,7 @@ int rnn_graph_create(const rnn_node_desc* nodes, int32_t n_nodes, const rnn_edge
     std::string err;
     if (!build_plan(ns, es, g->plan, err)) { delete g; return fail(RNN_ERR_INVALID_GRAPH, err); }
     g->served.assign(g->plan.comps.size(), std::array<int, 2>{0, 0});
+    g->layer_settings.resize(g->plan.layers.size());
     g->grad_groups.reserve(g->plan.grad_gemms.size() / GEMM_MAX_PROBLEMS + 1);
     g->grad_owned.reserve(g->plan.grad_gemms.size());
     if (const char* env = std::getenv("RNNG_SPIN_LIMIT")) g->spin_limit = std::max(1, std::atoi(env));
@@ -1192,6 +1245,12 @@ int rnn_graph_create(const rnn_node_desc* nodes, int32_t n_nodes, const rnn_edge
     if (const char* env = std::getenv("RNNG_CHAIN")) g->use_chains = std::atoi(env) != 0;
     if (const char* env = std::getenv("RNNG_STEP_BUILD")) g->prefer_streaming = std::string(env) == "stream";
     if (const char* env = std::getenv("RNNG_SCHEDULE")) g->framewise = std::string(env) == "framewise";
+    if (g->framewise)
+        for (const LayerPlan& lp : g->plan.layers)
+            if (lp.kind == NODE_ATTENTION) {
+                delete g;
+                return fail(RNN_ERR_INVALID_GRAPH, "an attention node's gradients need all frames of a window at once: not with RNNG_SCHEDULE=framewise");
+            }
     if (const char* env = std::getenv("RNNG_LAYOUT_SKEW")) g_layout_skew = std::atoll(env) / 256 * 256;
     if (const char* env = std::getenv("RNNG_BUNDLE"))
         if (std::atoi(env) == 0) g->plan.bundle_of.assign(g->plan.bundle_of.size(), -1);      // tuning aid: no exchange bundles
@@ -1246,6 +1305,7 @@ int64_t rnn_workspace_bytes(const rnn_graph* g, int32_t T, int32_t N) {
     if (!g) return fail(RNN_ERR_INVALID_ARGUMENT, "graph is NULL");
     if (T <= 0 || N <= 0) return fail(RNN_ERR_INVALID_ARGUMENT, "T and N must be positive");
     if ((int64_t)(T + g->plan.hist) * N >= (int64_t(1) << 31)) return fail(RNN_ERR_INVALID_ARGUMENT, "T * N exceeds 2^31 - 1");
+    if (const int rc = g->check_layers(T, N)) return rc;
     return const_cast<rnn_graph*>(g)->layout_for(T, N).total;
 }
 
@@ -1270,6 +1330,95 @@ int read_control(rnn_graph* g, double* loss, hipStream_t s) {
     return RNN_OK;
 }
 
+// ---- norm, attention and dropout layers: internal frames [t0, t1) of the current window -------
+RowTensor layer_rows(rnn_graph* g, int b, int t0) {
+    const int dim = g->plan.buf_dim[b];
+    return RowTensor{g->buf(b) + (int64_t)t0 * g->N * dim, dim};
+}
+rnn_frames layer_heads(rnn_graph* g, int b, int t0, int heads) {
+    const int64_t dim = g->plan.buf_dim[b];
+    return rnn_frames{g->buf(b) + (int64_t)t0 * g->N * dim, (int64_t)g->N * dim, dim, dim / heads};
+}
+float* layer_scratch(rnn_graph* g) { return g->layout.scratch_off < 0 ? nullptr : reinterpret_cast<float*>(g->ws + g->layout.scratch_off); }
+int64_t* passed_rows(rnn_graph* g) { return reinterpret_cast<int64_t*>(g->ws + g->layout.passed_off); }
+
+// The state of attention layer i behind frames [t0, t1), from `from` before them, to `to` (may be `from`); their outputs too, if with_outputs.
+int run_attention(rnn_graph* g, int i, const float* from, float* to, int t0, int t1, bool with_outputs, hipStream_t s) {
+    const Plan& P = g->plan;
+    const LayerPlan& lp = P.layers[i];
+    const rnn_linear_attention_desc d = g->attention_desc(i, t1 - t0, g->N);
+    rnn_frames x[3], o = layer_heads(g, P.ybuf(lp.node), t0, d.heads);
+    for (int j = 0; j < 3; ++j) x[j] = layer_heads(g, P.ybuf(lp.sums[j]), t0, d.heads);
+    return rnn_linear_attention_forward(&d, &x[0], &x[1], &x[2], g->layer_settings[i].d_log_decay, nullptr, from, to, with_outputs ? &o : nullptr,
+                                        layer_scratch(g), rnn_linear_attention_workspace_bytes(&d, 0), s);
+}
+DropoutRowsArgs layer_dropout(rnn_graph* g, int i, int from, int to, int t0, int t1) {
+    const rnn_graph::LayerSetting& ls = g->layer_settings[i];
+    return DropoutRowsArgs{(int64_t)(t1 - t0) * g->N, g->plan.buf_dim[from], dropout_args(ls.p, ls.seed, ls.offset, ls.d_offset), layer_rows(g, from, t0),
+                           layer_rows(g, to, t0), (int64_t)(t0 - g->hist()) * g->N, passed_rows(g)};
+}
+int layer_forward(rnn_graph* g, int i, int t0, int t1, hipStream_t s) {
+    const Plan& P = g->plan;
+    const LayerPlan& lp = P.layers[i];
+    const int prof = g->prof.begin(RNN_PROF_OTHER, s);
+    hipError_t e = hipSuccess;
+    if (lp.kind == NODE_ATTENTION) {
+        float* start = reinterpret_cast<float*>(g->ws + g->layout.state_off[i]);
+        float* reached = reinterpret_cast<float*>(g->ws + g->layout.reached_off[i]);
+        const int H = g->hist();
+        int rc = RNN_OK;
+        if (t0 > H && g->attention_upto != t0 - H) rc = run_attention(g, i, start, reached, H, t0, false, s);
+        if (rc == RNN_OK) rc = run_attention(g, i, t0 > H ? reached : start, reached, t0, t1, true, s);
+        if (rc != RNN_OK) return rc;
+    } else if (lp.kind == NODE_NORM) {
+        AddNormArgs a = {};
+        a.rows = (int64_t)(t1 - t0) * g->N; a.dim = P.xnodes[lp.node].dim; a.eps = RNN_NORM_EPS;
+        a.x = layer_rows(g, P.ybuf(lp.sums[0]), t0); a.y = layer_rows(g, P.ybuf(lp.node), t0);
+        a.gain = P.nodes[lp.node].has_bias ? g->weights + P.bias_off[lp.node] : nullptr;
+        a.rstd = static_cast<float*>(layer_rows(g, P.abuf(lp.node), t0).p);
+        e = launch_add_norm(DT_F32, a, s);
+    } else {
+        e = launch_dropout(DT_F32, layer_dropout(g, i, P.ybuf(lp.sums[0]), P.ybuf(lp.node), t0, t1), s);
+    }
+    g->prof.end(prof, 1, s);
+    return e == hipSuccess ? RNN_OK : fail_hip(e, "layer");
+}
+AddNormGradArgs norm_grad_args(rnn_graph* g, int i, int t0, int t1) {
+    const Plan& P = g->plan;
+    const LayerPlan& lp = P.layers[i];
+    AddNormGradArgs a = {};
+    a.rows = (int64_t)(t1 - t0) * g->N; a.dim = P.xnodes[lp.node].dim;
+    a.dy = layer_rows(g, P.dbuf(lp.node), t0); a.h = layer_rows(g, P.ybuf(lp.sums[0]), t0);
+    a.gain = P.nodes[lp.node].has_bias ? g->weights + P.bias_off[lp.node] : nullptr;
+    a.rstd = static_cast<float*>(layer_rows(g, P.abuf(lp.node), t0).p);
+    a.blocks = norm_grad_blocks(a.rows, a.dim);
+    return a;
+}
+// From the error terms of the layer's output to those of what its connections sum up to.
+int layer_backward(rnn_graph* g, int i, int t0, int t1, hipStream_t s) {
+    const Plan& P = g->plan;
+    const LayerPlan& lp = P.layers[i];
+    const int prof = g->prof.begin(RNN_PROF_OTHER, s);
+    hipError_t e = hipSuccess;
+    if (lp.kind == NODE_ATTENTION) {
+        const rnn_linear_attention_desc d = g->attention_desc(i, t1 - t0, g->N);
+        rnn_frames x[3], dx[3], d_o = layer_heads(g, P.dbuf(lp.node), t0, d.heads);
+        for (int j = 0; j < 3; ++j) { x[j] = layer_heads(g, P.ybuf(lp.sums[j]), t0, d.heads); dx[j] = layer_heads(g, P.dbuf(lp.sums[j]), t0, d.heads); }
+        const int rc = rnn_linear_attention_backward(&d, &x[0], &x[1], &x[2], g->layer_settings[i].d_log_decay, nullptr,
+                                                     reinterpret_cast<float*>(g->ws + g->layout.state_off[i]), &d_o, nullptr, &dx[0], &dx[1], &dx[2], nullptr,
+                                                     layer_scratch(g), rnn_linear_attention_workspace_bytes(&d, 1), s);
+        if (rc != RNN_OK) return rc;
+    } else if (lp.kind == NODE_NORM) {
+        AddNormGradArgs a = norm_grad_args(g, i, t0, t1);
+        a.dresidual = layer_rows(g, P.dbuf(lp.sums[0]), t0);
+        e = launch_add_norm_grad(DT_F32, a, s);
+    } else {
+        e = launch_dropout(DT_F32, layer_dropout(g, i, P.dbuf(lp.node), P.dbuf(lp.sums[0]), t0, t1), s);
+    }
+    g->prof.end(prof, 1, s);
+    return e == hipSuccess ? RNN_OK : fail_hip(e, "layer gradient");
+}
+
 // Forward pass over internal frames [t0, t1) of the current window: components in schedule order.
 int forward_frames(rnn_graph* g, int t0, int t1, hipStream_t s) {
     const Plan& P = g->plan;
@@ -1277,6 +1426,10 @@ int forward_frames(rnn_graph* g, int t0, int t1, hipStream_t s) {
     hipError_t e;
     int chain_done_to = -1;   // components up to this index were run as a chain
     for (const CompPlan& cp : P.comps) {
+        if (cp.layer >= 0) {
+            const int rc = layer_forward(g, cp.layer, t0, t1, s);
+            if (rc != RNN_OK) return rc;
+        }
         if (!cp.has_fwd_program) continue;
         const int c = (int)(&cp - P.comps.data());
         if (c <= chain_done_to) continue;
@@ -1320,6 +1473,7 @@ int rnn_forward_range(rnn_graph* g, const float* d_weights, const float* const* 
         if (!d_inputs[i] && !g->is_onehot(P.input_nodes[i])) return fail(RNN_ERR_INVALID_ARGUMENT, "an input tensor pointer is NULL");
     if (!d_workspace) return fail(RNN_ERR_WORKSPACE, "workspace is NULL");
     if (reinterpret_cast<uintptr_t>(d_workspace) & 255) return fail(RNN_ERR_WORKSPACE, "workspace is not 256-byte aligned");
+    if (const int rc = g->check_layers(T, N)) return rc;
     if (ws_bytes < g->layout_for(T, N).total)
         return fail(RNN_ERR_WORKSPACE, "workspace too small: need " + std::to_string(g->layout_for(T, N).total) + " bytes");
     if (g->cu_count == 0) {
@@ -1397,6 +1551,11 @@ int rnn_forward_range(rnn_graph* g, const float* d_weights, const float* const* 
         if (e != hipSuccess) return fail_hip(e, "window reset");
         g->prefilled = few;
         g->xcd_fields_used = 0;
+        // ... and the layers' states
+        for (size_t i = 0; i < P.layers.size() && e == hipSuccess; ++i)
+            if (L.state_off[i] >= 0) e = launch_fill(reinterpret_cast<float*>(g->ws + L.state_off[i]), (L.reached_off[i] - L.state_off[i]) / 4, 0.0f, s);
+        if (e == hipSuccess && L.passed_off >= 0) e = launch_count(passed_rows(g), 0, true, s);
+        if (e != hipSuccess) return fail_hip(e, "layer state reset");
     }
     // one-hot inputs with delayed connections: their class indices likewise (-1, the zero vector, in a fresh window's history)
     for (size_t i = 0; i < P.input_nodes.size(); ++i) {
@@ -1429,9 +1588,9 @@ int rnn_forward_range(rnn_graph* g, const float* d_weights, const float* const* 
     } else {
         const int rc = forward_frames(g, H + t_begin, H + t_end, s);
         g->prefilled = false;
-        if (rc != RNN_OK) return rc;
+        if (rc != RNN_OK) { g->attention_upto = -1; return rc; }
     }
-    g->fwd_upto = t_end;
+    g->fwd_upto = g->attention_upto = t_end;
     g->fwd_done = t_end == T;
     return RNN_OK;
 }
@@ -1463,6 +1622,7 @@ int rnn_forward_static(rnn_graph* g, const float* d_weights, const float* const*
         if (!d_outputs[i]) return fail(RNN_ERR_INVALID_ARGUMENT, "an output tensor pointer is NULL");
     if (T <= 0 || N <= 0) return fail(RNN_ERR_INVALID_ARGUMENT, "T and N must be positive");
     if (g->prof.mask != 0) return fail(RNN_ERR_SEQUENCE, "kernel-class timing creates events: switch it off for rnn_forward_static");
+    if (const int rc = g->check_layers(T, N)) return rc;
     const int64_t total = g->layout_for(T, N).total, need = total - g->layout_for(T, N).uncounted_bytes;
     const bool large = total > (int64_t)RNN_STATIC_WORKSPACE_BYTES;
     if (need > (int64_t)RNN_STATIC_WORKSPACE_BYTES)
@@ -1512,6 +1672,38 @@ int rnn_set_onehot_input(rnn_graph* g, int32_t input, const int32_t* d_indices) 
     return RNN_OK;
 }
 
+int rnn_set_attention(rnn_graph* g, int32_t node, int32_t heads, float scale, const float* d_log_decay) {
+    if (!g) return fail(RNN_ERR_INVALID_ARGUMENT, "graph is NULL");
+    for (size_t i = 0; i < g->plan.layers.size(); ++i) {
+        if (g->plan.layers[i].node != node || g->plan.layers[i].kind != NODE_ATTENTION) continue;
+        const int dim = g->plan.nodes[node].dim;
+        if (heads < 1 || dim % heads != 0 || dim / heads > ATTN_MAX_DIM)
+            return fail(RNN_ERR_INVALID_ARGUMENT, "heads must divide the node's units into heads of at most " + std::to_string(ATTN_MAX_DIM));
+        if (!std::isfinite(scale)) return fail(RNN_ERR_INVALID_ARGUMENT, "scale must be finite");
+        if (!d_log_decay || (reinterpret_cast<uintptr_t>(d_log_decay) & 3)) return fail(RNN_ERR_INVALID_ARGUMENT, "log_decay pointer is NULL or not aligned");
+        rnn_graph::LayerSetting& ls = g->layer_settings[i];
+        ls.heads = heads; ls.scale = scale; ls.d_log_decay = d_log_decay;
+        g->cached_T = g->cached_N = 0;      // (the heads' states have other sizes)
+        g->fwd_done = g->bptt_done = false; g->fwd_upto = 0;
+        return RNN_OK;
+    }
+    return fail(RNN_ERR_INVALID_ARGUMENT, "not an attention node");
+}
+
+int rnn_set_dropout(rnn_graph* g, int32_t node, float p, uint64_t seed, uint64_t offset, const uint64_t* d_offset) {
+    if (!g) return fail(RNN_ERR_INVALID_ARGUMENT, "graph is NULL");
+    for (size_t i = 0; i < g->plan.layers.size(); ++i) {
+        if (g->plan.layers[i].node != node || g->plan.layers[i].kind != NODE_DROPOUT) continue;
+        if (!(p >= 0.0f && p <= 1.0f)) return fail(RNN_ERR_INVALID_ARGUMENT, "the dropout probability must lie in [0, 1]");
+        if (reinterpret_cast<uintptr_t>(d_offset) & 7) return fail(RNN_ERR_INVALID_ARGUMENT, "offset pointer is not aligned");
+        rnn_graph::LayerSetting& ls = g->layer_settings[i];
+        ls.p = p; ls.seed = seed; ls.offset = offset; ls.d_offset = d_offset;
+        g->fwd_done = g->bptt_done = false; g->fwd_upto = 0;
+        return RNN_OK;
+    }
+    return fail(RNN_ERR_INVALID_ARGUMENT, "not a dropout node");
+}
+
 int rnn_shift_window(rnn_graph* g, int32_t frames, void* hip_stream) {
     if (!g) return fail(RNN_ERR_INVALID_ARGUMENT, "graph is NULL");
     if (!g->ws || g->fwd_upto != g->T) return fail(RNN_ERR_SEQUENCE, "rnn_shift_window needs a completely computed window");
@@ -1531,6 +1723,15 @@ int rnn_shift_window(rnn_graph* g, int32_t frames, void* hip_stream) {
         return e;
     };
     hipError_t e = hipSuccess;
+    // the layers: states at the new window's start, from the frames that leave it
+    for (size_t i = 0; i < P.layers.size(); ++i)
+        if (P.layers[i].kind == NODE_ATTENTION) {
+            float* start = reinterpret_cast<float*>(g->ws + g->layout.state_off[i]);
+            if (const int rc = run_attention(g, (int)i, start, start, g->hist(), g->hist() + frames, false, s)) { g->fwd_upto = 0; return rc; }
+        } else if (P.layers[i].kind == NODE_NORM && e == hipSuccess) {
+            e = shift(g->buf(P.abuf(P.layers[i].node)), g->N);
+        }
+    if (!P.layers.empty() && e == hipSuccess) e = launch_count(passed_rows(g), (int64_t)frames * g->N, false, s);
     for (size_t k = 0; k < P.xnodes.size() && e == hipSuccess; ++k) {
         const int b = P.ybuf((int)k);
         if (g->layout.buf_off[b] < 0) continue;      // an input read in place: the caller shifts it
@@ -1547,7 +1748,7 @@ int rnn_shift_window(rnn_graph* g, int32_t frames, void* hip_stream) {
         if (e == hipSuccess && bp.members[0] < (int)P.xnodes.size() && g->layout.buf_off[bp.ebuf] >= 0) e = shift(g->buf(bp.ebuf), P.frame_floats(bp.ebuf, g->N));
     if (e == hipSuccess) e = launch_shift_frames(st, frames, Ti, s);
     if (e != hipSuccess) return fail_hip(e, "window shift");
-    g->fwd_upto = g->T - frames;
+    g->fwd_upto = g->attention_upto = g->T - frames;
     g->fwd_done = g->bptt_done = false;
     return RNN_OK;
 }
@@ -1613,6 +1814,10 @@ int rnn_bptt(rnn_graph* g, const float* d_weights, const void* const* d_targets,
             if (e != hipSuccess) return fail_hip(e, "backward GEMM");
             const StepRun r = run_phases(g, c, true, s, t0, t1);
             if (r.error) return fail(RNN_ERR_DEVICE, "backward: " + r.err);
+            if (cp.layer >= 0) {
+                const int rc = layer_backward(g, cp.layer, t0, t1, s);
+                if (rc != RNN_OK) return rc;
+            }
         }
         return RNN_OK;
     };
@@ -1637,7 +1842,10 @@ int rnn_state_grad(const rnn_graph* g, int32_t node, const float** d_ds) {
     if (node < 0 || node >= (int)g->plan.nodes.size()) return fail(RNN_ERR_INVALID_ARGUMENT, "node index out of range");
     if (g->plan.nodes[node].kind == NODE_INPUT) return fail(RNN_ERR_INVALID_ARGUMENT, "input nodes have no state gradient");
     if (!g->bptt_done) return fail(RNN_ERR_SEQUENCE, "rnn_state_grad before rnn_bptt");
-    *d_ds = g->frame0(g->plan.dbuf(node));
+    int k = node;
+    for (const LayerPlan& lp : g->plan.layers)
+        if (lp.node == node && lp.kind != NODE_ATTENTION) k = lp.sums[0];
+    *d_ds = g->frame0(g->plan.dbuf(k));
     return RNN_OK;
 }
 
@@ -1736,6 +1944,13 @@ int rnn_grads(rnn_graph* g, float* d_grads, double* loss, void* hip_stream) {
     g->prof.end(prof, n_launch, s);
     e = launch_colsum(g->view(), P.colsum_off, P.n_colsum, P.colsum_max_dim, g->weights, d_grads, H + T, N, H, g->deterministic, s);
     if (e != hipSuccess) return fail_hip(e, "diagonal / bias gradient");
+    for (size_t i = 0; i < P.layers.size(); ++i) {
+        if (P.layers[i].kind != NODE_NORM || !P.nodes[P.layers[i].node].has_bias) continue;
+        AddNormGradArgs a = norm_grad_args(g, (int)i, H, H + T);      // the gain's alone
+        a.dgain = d_grads + P.bias_off[P.layers[i].node]; a.partial = layer_scratch(g);
+        e = launch_add_norm_grad(DT_F32, a, s);
+        if (e != hipSuccess) return fail_hip(e, "gain gradient");
+    }
     if (loss) return read_control(g, loss, s);
     return RNN_OK;
 }

@@ -602,10 +602,12 @@ static hipError_t launch_attention_steps(const AttnCall& c, const AttnOp* ops, i
 }
 
 // Segments of the frames, so that the chip is filled (two workgroups to a compute unit) where streams and heads are few.
-static void plan_segments(int T, int64_t works, int C, int& n_seg, int& seg_len) {
+static int64_t most_segments(int T, int64_t works, int C) {      // (grows with T: room for a window's is room for a part's)
     const int64_t chunks = (T + C - 1) / C;
-    int64_t n = works >= 256 ? 1 : std::min<int64_t>((512 + works - 1) / works, chunks / 4);
-    n = std::max<int64_t>(n, 1);
+    return std::max<int64_t>(1, works >= 256 || works == 0 ? 1 : std::min<int64_t>((512 + works - 1) / works, chunks / 4));
+}
+static void plan_segments(int T, int64_t works, int C, int& n_seg, int& seg_len) {
+    const int64_t chunks = (T + C - 1) / C, n = most_segments(T, works, C);
     const int64_t per = (chunks + n - 1) / n;
     seg_len = (int)(per * C);
     n_seg = std::max<int>(1, (int)((chunks + per - 1) / per));
@@ -631,8 +633,7 @@ int64_t attention_space(const AttnCall& c, const AttnOp* ops, int n_ops) {
     int64_t floats = 0;
     for (int i = 0; i < n_ops; ++i) { dk = std::max(dk, ops[i].dk); dv = std::max(dv, ops[i].dv); floats += ((int64_t)ops[i].dk * ops[i].dv * c.N * c.heads + 63) / 64 * 64; }
     const ChunkShape sh = chunk_shape(c.dtype, dk, dv);
-    int n_seg, seg_len;
-    plan_segments(c.T, (int64_t)c.N * c.heads * n_ops * sh.slices, sh.C, n_seg, seg_len);
+    const int64_t n_seg = most_segments(c.T, (int64_t)c.N * c.heads * n_ops * sh.slices, sh.C);
     return n_seg > 1 ? n_seg * floats * 4 : 0;
 }
 

@@ -9,7 +9,10 @@ namespace rnng {
 struct GNode { int kind, act, dim, has_bias, is_output; };
 struct GEdge { int src, dst, delay, wkind; };
 
-enum { NODE_INPUT = 0, NODE_ADD = 1, NODE_MUL = 2, NODE_MAX = 3 };
+enum { NODE_INPUT = 0, NODE_ADD = 1, NODE_MUL = 2, NODE_MAX = 3, NODE_NORM = 4, NODE_ATTENTION = 5, NODE_DROPOUT = 6 };
+// Kinds whose output unit depends on more than the same unit of its connections' outputs (or on its place in the sequence): kernels of
+// their own work on them for all frames at once, and they cannot lie inside a recurrent node.
+inline bool whole_frames(int kind) { return kind >= NODE_NORM && kind <= NODE_DROPOUT; }
 enum { ACT_LINEAR = 0, ACT_SIGMOID = 1, ACT_TANH = 2, ACT_SOFTMAX = 3, ACT_RELU = 4 };
 enum { OUT_NONE = 0, OUT_CROSS_ENTROPY = 1, OUT_SQUARED_ERROR = 2 };      // GNode::is_output
 enum { W_FULL = 0, W_DIAG = 1, W_IDENTITY = 2 };

@@ -27,10 +27,9 @@ inline DropoutArgs dropout_args(double p, uint64_t seed, uint64_t offset, const 
 constexpr int NORM_MAX_DIM = 16384;
 struct AddNormArgs {
     int64_t rows; int dim; float eps; DropoutArgs drop;
-    RowTensor x, residual, h, y;                      // residual, h: p may be NULL; first_row: the number of row 0 for dropout
+    RowTensor x, residual, h, y;                      // residual, h: p may be NULL
     const float* gain; float* rstd;
     float* scales; int group;                         // y in e4m3 with scales if scales != NULL
-    int64_t first_row;
 };
 hipError_t launch_add_norm(int dtype, const AddNormArgs& a, hipStream_t s);
 struct AddNormGradArgs {
@@ -38,12 +37,13 @@ struct AddNormGradArgs {
     RowTensor dy, dh, h, dx, dresidual;               // dh, dx, dresidual: p may be NULL
     const float* gain; const float* rstd; float* dgain; float* partial;
     int blocks;                                       // norm_grad_blocks: rows of `partial`
-    int64_t first_row;
 };
 int norm_grad_blocks(int64_t rows, int dim);
 hipError_t launch_add_norm_grad(int dtype, const AddNormGradArgs& a, hipStream_t s);
-struct DropoutRowsArgs { int64_t rows; int dim; DropoutArgs drop; RowTensor x, y; int64_t first_row; };
+// The generator's number of row 0 is first_row + *d_first_row (NULL: 0).
+struct DropoutRowsArgs { int64_t rows; int dim; DropoutArgs drop; RowTensor x, y; int64_t first_row; const int64_t* d_first_row; };
 hipError_t launch_dropout(int dtype, const DropoutRowsArgs& a, hipStream_t s);
+hipError_t launch_count(int64_t* p, int64_t add, bool fresh, hipStream_t s);      // *p = (fresh ? 0 : *p) + add
 
 // ---- linear attention with a decay for each head --------------------------------------------
 // One operator serves the forward pass and all of its gradients.  For stream n, head h and its L frames, with g = exp(log_decay[h]):

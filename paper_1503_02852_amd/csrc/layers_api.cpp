@@ -298,7 +298,7 @@ int rnn_dropout(const rnn_dropout_desc* d, const void* d_x, int64_t ld_x, void* 
         int rc = check_row_tensor("x", d_x, ld_x, d->rows, d->dim, b, true);
         if (!rc) rc = check_row_tensor("y", d_y, ld_y, d->rows, d->dim, b, true);
         if (rc) return rc;
-        const DropoutRowsArgs a{d->rows, d->dim, dropout_args(d->p, d->seed, d->offset, d->d_offset), RowTensor{const_cast<void*>(d_x), ld_x}, RowTensor{d_y, ld_y}, 0};
+        const DropoutRowsArgs a{d->rows, d->dim, dropout_args(d->p, d->seed, d->offset, d->d_offset), RowTensor{const_cast<void*>(d_x), ld_x}, RowTensor{d_y, ld_y}, 0, nullptr};
         return done(launch_dropout(d->dtype, a, static_cast<hipStream_t>(hip_stream)), "dropout launch");
     });
 }

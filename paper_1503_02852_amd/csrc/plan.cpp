@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <array>
 #include <map>
+#include <string>
 
 namespace rnng {
 
@@ -299,6 +300,11 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
     P.nodes = nodes; P.edges = edges;
     if (!analyse_graph(nodes, edges, P.sched, err)) return false;
     const int K0 = (int)nodes.size(), M0 = (int)edges.size();
+    for (int k = 0; k < K0; ++k)
+        if (whole_frames(nodes[k].kind) && P.sched.comp_recurrent[P.sched.node_comp[k]]) {
+            err = "node " + std::to_string(k) + ": a norm, attention or dropout node cannot be part of a recurrent node";
+            return false;
+        }
     for (int k = 0; k < K0; ++k) {
         if (nodes[k].kind == NODE_INPUT) P.input_nodes.push_back(k);
         if (nodes[k].is_output) P.output_nodes.push_back(k);
@@ -321,8 +327,22 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
     P.n_params = cur;
     if (cur >= (int64_t(1) << 31)) { err = "parameter count exceeds 2^31 - 1"; return false; }
 
-    // ---- execution graph: route full edges into multiplicative nodes through a linear node ----
+    // ---- execution graph: route full edges into multiplicative nodes through a linear node, all edges into norm, attention and dropout nodes likewise ----
     P.xnodes = nodes;
+    std::vector<int> layer_of(K0, -1);
+    for (int k = 0; k < K0; ++k)
+        if (whole_frames(nodes[k].kind)) {
+            layer_of[k] = (int)P.layers.size();
+            LayerPlan lp{nodes[k].kind, k, {-1, -1, -1}};
+            const int n_sums = nodes[k].kind == NODE_ATTENTION ? 3 : 1;
+            for (int i = 0; i < n_sums; ++i) {
+                lp.sums[i] = (int)P.xnodes.size();
+                P.xnodes.push_back(GNode{NODE_ADD, ACT_LINEAR, nodes[k].dim, 0, 0});
+                P.xedges.push_back(GEdge{lp.sums[i], k, 0, W_IDENTITY}); P.xedge_param.push_back(-1);
+            }
+            P.layers.push_back(lp);
+        }
+    std::vector<int> n_routed(K0, 0);
     for (int m = 0; m < M0; ++m) {
         const GEdge& e = edges[m];
         if (e.wkind == W_FULL && (nodes[e.dst].kind == NODE_MUL || nodes[e.dst].kind == NODE_MAX)) {
@@ -330,6 +350,9 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
             P.xnodes.push_back(GNode{NODE_ADD, ACT_LINEAR, nodes[e.dst].dim, 0, 0});
             P.xedges.push_back(GEdge{e.src, s, e.delay, W_FULL}); P.xedge_param.push_back(m);
             P.xedges.push_back(GEdge{s, e.dst, 0, W_IDENTITY}); P.xedge_param.push_back(-1);
+        } else if (layer_of[e.dst] >= 0) {
+            const LayerPlan& lp = P.layers[layer_of[e.dst]];
+            P.xedges.push_back(GEdge{e.src, lp.sums[lp.kind == NODE_ATTENTION ? n_routed[e.dst]++ : 0], e.delay, e.wkind}); P.xedge_param.push_back(m);
         } else {
             P.xedges.push_back(e); P.xedge_param.push_back(m);
         }
@@ -354,6 +377,11 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
         for (int b : {P.ybuf(k), P.dbuf(k), P.abuf(k), P.pbuf(k), P.qbuf(k), P.hbuf(k), P.fbuf(k)}) P.buf_dim[b] = xn[k].dim;
         if (xn[k].kind != NODE_INPUT) P.buf_alloc[P.ybuf(k)] = P.buf_alloc[P.dbuf(k)] = 1;
         else if (P.input_staged[k]) P.buf_alloc[P.ybuf(k)] = 1;
+    }
+    std::vector<char> sum_of_layer(K, 0);
+    for (const LayerPlan& lp : P.layers) {
+        for (int s : lp.sums) if (s >= 0) sum_of_layer[s] = 1;
+        if (lp.kind == NODE_NORM) { P.buf_dim[P.abuf(lp.node)] = 1; P.buf_alloc[P.abuf(lp.node)] = 1; }
     }
     // y_src of a full connection inside a recurrent node is read by all workgroups during the
     // forward step loop, ds_dst during the backward one
@@ -382,6 +410,8 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
             return S.node_level[a] != S.node_level[b] ? S.node_level[a] < S.node_level[b] : a < b;
         });
 
+        if (members[0] < K0) cp.layer = layer_of[members[0]];
+
         // phases: a delay-0 full edge inside the component separates its source and destination
         std::map<int, int> phase;
         int n_phases = 1;
@@ -404,7 +434,7 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
             if (xn[k].act == ACT_SOFTMAX) cp.softmax_node = k;
             else if (xn[k].is_output == OUT_SQUARED_ERROR) cp.sqerr_node = k;
         }
-        for (int p = 0; p < n_phases; ++p) {
+        for (int p = 0; p < (cp.layer >= 0 ? 0 : n_phases); ++p) {      // (a layer's forward pass is its kernel's alone)
             std::vector<int> np;
             for (int k : members) if (phase[k] == p) np.push_back(k);
             std::map<int, int> slot;
@@ -464,7 +494,7 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
             for (int k : members) if (shared_y[k]) shared[P.ybuf(k)] = 1;
             if (!emit_phase(P, cp.fwd_phases, tasks, ops, part_bufs, written, shared, cp.recurrent ? -1 : 0, err)) return false;
         }
-        cp.has_fwd_program = true;
+        cp.has_fwd_program = cp.layer < 0;
         if (!cp.recurrent && members.size() == 1 && xn[members[0]].kind == NODE_ADD && cp.fwd_gemms.size() == 1) {
             const int k = members[0];
             cp.in_products = cp.fwd_gemms[0].c_buf == P.ybuf(k);
@@ -482,6 +512,7 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
         if (fhelper && fhelper->has_fwd_program) fhelper->fwd_desc_off = emit_desc(fhelper->fwd_phases);
 
         // ---- backward ----
+        if (sum_of_layer[members[0]]) return true;                      // the layer's kernel writes its error terms
         if (cp.softmax_node >= 0 || cp.sqerr_node >= 0) return true;   // the output delta comes from the error-criterion kernel
         for (int j : members) {
             GemmProblemPlan gp; gp.c_buf = shared_d[j] ? P.qbuf(j) : P.dbuf(j); gp.n = xn[j].dim;
@@ -710,7 +741,7 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
         emit_colsum(xn[e.dst].dim, (int)full_off(m), fs);
     }
     for (int k = 0; k < K0; ++k)
-        if (nodes[k].has_bias) emit_colsum(nodes[k].dim, (int)P.bias_off[k], {FactorH{P.dbuf(k), 0, -1, -1}});
+        if (nodes[k].has_bias && nodes[k].kind != NODE_NORM) emit_colsum(nodes[k].dim, (int)P.bias_off[k], {FactorH{P.dbuf(k), 0, -1, -1}});
     return true;
 }
 

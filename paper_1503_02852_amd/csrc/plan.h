@@ -59,7 +59,12 @@ struct CompPlan {
     int64_t step_weight_floats = 0;         // weights of all full connections inside the component
     int chain = -1;                         // index into Plan::chains if the component is a chain member
     bool helper = false;                    // a helper member of a chain launch (ChainPlan::fwd_split / bwd_split)
+    int layer = -1;                         // index into Plan::layers if the component is such a node
 };
+
+// A norm, attention or dropout node.  Its connections lead into linear additive nodes of the execution graph, one for all of them or (attention)
+// one for each, whose activations its kernel reads and whose error terms it writes.  Norm: 1 / root mean square per row is kept in abuf(node).
+struct LayerPlan { int kind, node, sums[3]; };
 
 // Consecutive recurrent components first..last whose step loops can run side by side in one
 // kernel launch: members[i] is component first + i lowered with the full connections between
@@ -120,6 +125,7 @@ struct Plan {
     int twin_base = -1;
     std::vector<CompPlan> comps;
     std::vector<ChainPlan> chains;
+    std::vector<LayerPlan> layers;
     std::vector<BundlePlan> bundles;
     std::vector<int> bundle_of;             // per buffer id: index into bundles or -1
     std::vector<GradGemmPlan> grad_gemms;

@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) add_norm_kernel(AddNorm
         }
         if (a.drop.cut)
 #pragma unroll
-            for (int v = 0; v < NV; ++v) h[v] = drop8(h[v], (uint64_t)(r + a.first_row) * groups + v * TPR + lane, offset, a.drop);
+            for (int v = 0; v < NV; ++v) h[v] = drop8(h[v], (uint64_t)r * groups + v * TPR + lane, offset, a.drop);
         if (a.residual.p)
 #pragma unroll
             for (int v = 0; v < NV; ++v) h[v] += res[v];
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) add_norm_grad_kernel(Ad
             if (a.dh.p) s += dh[v];
             if (a.dresidual.p) store8<WHOLE>((T*)a.dresidual.p + r * a.dresidual.ld + at, s, dim - at);
             if (a.dx.p) {
-                if (a.drop.cut) s = drop8(s, (uint64_t)(r + a.first_row) * groups + v * TPR + lane, offset, a.drop);
+                if (a.drop.cut) s = drop8(s, (uint64_t)r * groups + v * TPR + lane, offset, a.drop);
                 store8<WHOLE>((T*)a.dx.p + r * a.dx.ld + at, s, dim - at);
             }
         }
@@ -277,12 +277,15 @@ __global__ void __launch_bounds__(256) zero_kernel(float* p, int n) {
     if (i < n) p[i] = 0.0f;
 }
 
+__global__ void count_kernel(int64_t* p, int64_t add, bool fresh) { *p = (fresh ? 0 : *p) + add; }
+
 // A thread takes groups of eight units, four of them in flight.
 template <class T, bool WHOLE>
 __global__ void __launch_bounds__(256) dropout_kernel(DropoutRowsArgs a) {
     constexpr int U = 4;
     const unsigned groups = (unsigned)(a.dim + 7) / 8;
     const uint64_t total = (uint64_t)a.rows * groups, offset = drop_offset(a.drop);
+    const int64_t first_row = a.first_row + (a.d_first_row ? *a.d_first_row : 0);
     for (uint64_t base = (uint64_t)blockIdx.x * (256 * U); base < total; base += (uint64_t)gridDim.x * (256 * U)) {
         f32x8 x[U];
         int64_t row[U]; int at[U];
@@ -299,7 +302,7 @@ __global__ void __launch_bounds__(256) dropout_kernel(DropoutRowsArgs a) {
         for (int u = 0; u < U; ++u) {
             if (at[u] >= a.dim) continue;
             f32x8 y = x[u];
-            if (a.drop.cut) y = drop8(y, (uint64_t)(row[u] + a.first_row) * groups + at[u] / 8, offset, a.drop);
+            if (a.drop.cut) y = drop8(y, (uint64_t)(row[u] + first_row) * groups + at[u] / 8, offset, a.drop);
             store8<WHOLE>((T*)a.y.p + row[u] * a.y.ld + at[u], y, a.dim - at[u]);
         }
     }
@@ -368,6 +371,11 @@ hipError_t launch_add_norm_grad(int dtype, const AddNormGradArgs& a, hipStream_t
         e = hipGetLastError();
     }
     return e;
+}
+
+hipError_t launch_count(int64_t* p, int64_t add, bool fresh, hipStream_t s) {
+    count_kernel<<<1, 1, 0, s>>>(p, add, fresh);
+    return hipGetLastError();
 }
 
 hipError_t launch_dropout(int dtype, const DropoutRowsArgs& a, hipStream_t s) {

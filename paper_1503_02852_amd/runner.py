@@ -11,12 +11,19 @@ from .binding import Graph
 class Window:
     """One graph + one window shape (T, N) with all device buffers allocated."""
 
-    def __init__(self, node_array, edge_array, T, N, device="cuda:0"):
+    def __init__(self, node_array, edge_array, T, N, device="cuda:0", attention=None):
+        """attention: {node: (heads, scale, log_decay [heads])} for the attention nodes."""
         if not torch.cuda.is_available():
             raise RuntimeError("rnngraph needs a GPU: there is no CPU path")
         self.g = Graph(node_array, edge_array)
         self.T, self.N = T, N
         self.dev = torch.device(device)
+        self.log_decay = {}
+        for k, (heads, scale, log_decay) in (attention or {}).items():
+            a = np.ascontiguousarray(log_decay, dtype=np.float32)
+            assert a.shape == (heads,), a.shape
+            self.log_decay[k] = torch.from_numpy(a).to(self.dev)
+            self.g.set_attention(k, heads, self.log_decay[k].data_ptr(), scale)
         self.ws_bytes = self.g.workspace_bytes(T, N)
         self.ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.dev)
         self.ws_ptr = (self.ws.data_ptr() + 255) // 256 * 256
@@ -128,7 +135,12 @@ class Window:
 
 
 def window_for(workload, device="cuda:0"):
-    w = Window(workload.spec.node_array(), workload.spec.edge_array(), workload.T, workload.N, device)
+    nodes = workload.spec.nodes
+    w = Window(workload.spec.node_array(), workload.spec.edge_array(), workload.T, workload.N, device,
+               {k: (n["heads"], n["scale"], n["log_decay"]) for k, n in enumerate(nodes) if "heads" in n})
+    for k, n in enumerate(nodes):
+        if "dropout" in n:
+            w.g.set_dropout(k, *n["dropout"])
     w.set_params(workload.weights, workload.biases)
     w.set_inputs(workload.inputs)
     w.set_targets(workload.targets)

@@ -7,7 +7,8 @@ layer, an edge is a connection with a weight matrix and a delay) and (b) seeded
 random weights, inputs and targets.
 
 Enumerations are the interface's integer codes (they appear in the C header too):
-  node kind : 0 input, 1 additive, 2 multiplicative, 3 element-wise maximum
+  node kind : 0 input, 1 additive, 2 multiplicative, 3 element-wise maximum, 4 root-mean-square norm,
+              5 linear attention with decays, 6 dropout
   activation: 0 linear, 1 logistic sigmoid, 2 tanh, 3 softmax (output nodes only), 4 rectifier max(0, s)
   weight kind: 0 full matrix [n_dst x n_src], 1 diagonal (vector), 2 identity
   is_output : 0 no, 1 softmax output with class targets (cross-entropy), 2 output with dense
@@ -17,7 +18,7 @@ from __future__ import annotations
 
 import numpy as np
 
-INPUT, ADD, MUL, MAX = 0, 1, 2, 3
+INPUT, ADD, MUL, MAX, NORM, ATTENTION, DROPOUT = 0, 1, 2, 3, 4, 5, 6
 LINEAR, SIGMOID, TANH, SOFTMAX, RELU = 0, 1, 2, 3, 4
 FULL, DIAG, IDENTITY = 0, 1, 2
 CROSS_ENTROPY, SQUARED_ERROR = 1, 2
@@ -27,13 +28,14 @@ class GraphSpec:
     """A network as a plain node list and edge list."""
 
     def __init__(self):
-        self.nodes = []   # dicts: kind, act, dim, has_bias, is_output, name
+        self.nodes = []   # dicts: kind, act, dim, has_bias, is_output, name; attention nodes also heads, scale and
+                          # log_decay [heads], dropout nodes dropout = (p, seed, offset)
         self.edges = []   # dicts: src, dst, delay, wkind
 
-    def add_node(self, kind, act, dim, has_bias=False, is_output=False, name=""):
+    def add_node(self, kind, act, dim, has_bias=False, is_output=False, name="", **layer):
         self.nodes.append(dict(kind=int(kind), act=int(act), dim=int(dim),
                                has_bias=int(bool(has_bias)), is_output=int(is_output),
-                               name=name or f"n{len(self.nodes)}"))
+                               name=name or f"n{len(self.nodes)}", **layer))
         return len(self.nodes) - 1
 
     def add_edge(self, src, dst, wkind, delay=0):
@@ -138,6 +140,44 @@ def lstm_net(n_in, hidden, n_out, output_recurrence=True, squared_error_act=None
     return g
 
 
+def attention_net(n_in, dim, heads, n_layers, n_out, dropout=0.0, seed=1):
+    """A residual stream of dim units with, layer by layer, norm -> linear attention (head h forgets with exp(-2^-(h + 2))) -> full
+    connection -> dropout and norm -> rectifier layer of 2 dim units -> full connection -> dropout added to it; a last norm; softmax."""
+    g = GraphSpec()
+    x = g.add_node(INPUT, LINEAR, n_in, name="x")
+    top = g.add_node(ADD, LINEAR, dim, name="embed")
+    g.add_edge(x, top, FULL)
+
+    def norm(name):
+        k = g.add_node(NORM, LINEAR, dim, has_bias=True, name=name)
+        g.add_edge(top, k, IDENTITY)
+        return k
+
+    def joined(branch, name, number):
+        b = g.add_node(ADD, LINEAR, dim, name=name + "_branch")
+        d = g.add_node(DROPOUT, LINEAR, dim, name=name + "_drop", dropout=(dropout, seed, number))
+        s = g.add_node(ADD, LINEAR, dim, name=name)
+        g.add_edge(branch, b, FULL)
+        g.add_edge(b, d, IDENTITY)
+        g.add_edge(top, s, IDENTITY)
+        g.add_edge(d, s, IDENTITY)
+        return s
+
+    for i in range(n_layers):
+        a = g.add_node(ATTENTION, LINEAR, dim, name=f"A{i + 1}", heads=heads, scale=(dim // heads) ** -0.5,
+                       log_decay=-2.0 ** -(np.arange(heads) % 8 + 2.0))
+        n = norm(f"A{i + 1}_norm")
+        for _ in range(3):
+            g.add_edge(n, a, FULL)
+        top = joined(a, f"A{i + 1}_sum", 2 * i)
+        f = g.add_node(ADD, RELU, 2 * dim, has_bias=True, name=f"F{i + 1}")
+        g.add_edge(norm(f"F{i + 1}_norm"), f, FULL)
+        top = joined(f, f"F{i + 1}_sum", 2 * i + 1)
+    out = g.add_node(ADD, SOFTMAX, n_out, has_bias=True, is_output=CROSS_ENTROPY, name="out")
+    g.add_edge(norm("out_norm"), out, FULL)
+    return g
+
+
 def elman_net(n_in, n_hidden, n_out, act=TANH):
     """Elman network: one hidden layer with a delay-1 full self-loop (Section 4's other net)."""
     g = GraphSpec()
@@ -233,7 +273,7 @@ def random_graph(rng, n_inner=6, max_dim=5, p_edge=0.35, max_delay=3, n_inputs=1
 def draw_params(spec, rng, scale, bias_scale=0.0):
     """Weights per edge (index order): FULL -> [n_dst, n_src], DIAG -> [dim], IDENTITY -> None,
     uniform in (-scale, scale), float32.  Biases per node (index order): zeros unless
-    bias_scale > 0."""
+    bias_scale > 0; a norm node's gains are 1 more."""
     weights, biases = [], []
     for e in spec.edges:
         ns, nd = spec.nodes[e["src"]]["dim"], spec.nodes[e["dst"]]["dim"]
@@ -249,6 +289,8 @@ def draw_params(spec, rng, scale, bias_scale=0.0):
                 biases.append(rng.uniform(-bias_scale, bias_scale, size=(n["dim"],)).astype(np.float32))
             else:
                 biases.append(np.zeros((n["dim"],), dtype=np.float32))
+            if n["kind"] == NORM:
+                biases[-1] += np.float32(1)
         else:
             biases.append(None)
     return weights, biases
@@ -343,6 +385,8 @@ def make_config(name, seed=0, T=None, N=None, bias_scale=0.0):
         spec, T0, N0, a, kind = elman_net(38000, 512, 20000), 2048, 1, 0.05, "words"
     elif name == "lm_lstm_n1":       # Section 4: LSTM without the block-output -> gate recurrence, same sizes
         spec, T0, N0, a, kind = lstm_net(38000, [512], 20000, output_recurrence=False), 2048, 1, 0.05, "words"
+    elif name == "charlm_attention_n32":      # the character model with linear attention instead of LSTM layers
+        spec, T0, N0, a, kind = attention_net(30, 512, 4, 2, 30, dropout=0.1), 256, 32, 0.08, "symbols"
     elif name.startswith("fig4_h"):
         H, N0 = (int(v) for v in name[len("fig4_h"):].split("_n"))
         spec, T0, a, kind = lstm_net(H, [H], H), 2048 // N0, 0.02, "gauss"
