@@ -228,6 +228,7 @@ def main():
         sys.exit(2)
 
     import torch
+    import workloads as wl
     from paper_1503_02852_amd.runner import window_for
 
     m = measure(args.workload, args.steps, args.warmup, args.index_input, args.calibrate_copy)
@@ -253,7 +254,7 @@ def main():
         out["paper_schedule"] = dict(value=p["value"], unit="frames/s", ms_per_step=p["ms_per_step"], schedule=p["schedule"],
                                      roofline_frac=p["roofline"]["frac"], batched_gemms=p["gemms"])
         del p
-    if not args.no_framewise:
+    if not args.no_framewise and not w.spec.has(wl.ATTENTION):      # (whose gradients need all frames of a window)
         # Section 4's baseline on the same kernels' per-frame forms: every frame on its own, no batching
         # over frames, no persistent step kernel.  Reported next to the paper's ">10x" for its own schedule.
         os.environ["RNNG_SCHEDULE"] = "framewise"

@@ -57,6 +57,9 @@ class GraphSpec:
     def output_nodes(self):
         return [k for k, n in enumerate(self.nodes) if n["is_output"]]
 
+    def has(self, kind):
+        return any(n["kind"] == kind for n in self.nodes)
+
     def node_by_name(self, name):
         for k, n in enumerate(self.nodes):
             if n["name"] == name:
