@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
     const T* lds_k = lds_ks;
     const T* lds_v = lds_vs;
     if (begin < end) {
-        if constexpr (!STATE) tq.load(lds_q, end - begin);
+        if constexpr (!STATE) if (a.o.p) tq.load(lds_q, end - begin);                 // (without outputs there may be no q)
         tk.load(lds_ks, end - begin);
         tv.load(lds_vs, end - begin);
     }

@@ -171,6 +171,9 @@ def test_attention_without_state_and_single_outputs(T):
     only = torch.empty_like(c.state_out)
     c.layer.forward(x["q"], x["k"], x["v"], c.log_decay, None, state_out=only, lengths=c.lengths)      # the state alone
     assert torch.equal(only, c.state_out)
+    only.fill_(c.MARK)
+    c.layer.forward(None, x["k"], x["v"], c.log_decay, None, state_out=only, lengths=c.lengths)
+    assert torch.equal(only, c.state_out)
     o = torch.full_like(x["o"], c.MARK)
     c.layer.forward(x["q"], x["k"], x["v"], c.log_decay, o, lengths=c.lengths)
     assert torch.equal(o, x["o"])
@@ -249,6 +252,85 @@ def test_attention_same_bits_again_on_other_streams_and_captured(T):
         same()
         c.forward()      # the program's own call between the replays
         same()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_state_alone_over_many_frames(dtype):
+    """In segments, without q."""
+    c = Attention(3000, 1, 2, 1, 64, 32, dtype, seed=2, decays=[-1e-3, -0.2])
+    c.layer.forward(None, c.x["k"], c.x["v"], c.log_decay, None, state=c.state, state_out=c.state_out)
+    c.check(("state_out",), False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [3, 40])
+def test_attention_offsets_beyond_32_bits(T, dtype):
+    """Frames so far apart that the last one lies 2^31 elements behind the first."""
+    c = Attention(T, 2, 4, 2, 48, 64, dtype, seed=T)
+    step = -(-(1 << 31) // (T - 1)) // 64 * 64 + 4096
+    big = torch.empty((T - 1) * step + 4096 * 16, device=DEV, dtype=c.t)
+    at = 0
+    for name, x in c.x.items():
+        far = big[at:].as_strided(x.shape, (step,) + x.stride()[1:])
+        far.copy_(x)
+        c.x[name] = far
+        at += x[0].numel() + 16
+    assert at <= 4096 and (T - 1) * step >= 1 << 31
+    c.forward()
+    c.check(("o", "state_out"), False)
+    c.backward()
+    c.check(("dq", "dk", "dv", "dstate"), True)
+
+
+@pytest.mark.parametrize("T", [3, 150, 2500])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_attention_keeps_infinities_to_their_stream_and_head(T, bad):
+    from paper_1503_02852_amd import layers
+    r = np.random.default_rng(1)
+    f = lambda *s: torch.from_numpy(r.standard_normal(s).astype(np.float32)).to(DEV).to(torch.bfloat16)  # noqa: E731
+    q, k, v, do = (f(T, 2, 3, 32) for _ in range(4))
+    decay = torch.tensor([-0.1, -0.01, 0.0], device=DEV)
+    layer = layers.LinearAttention(T, 2, 3, 32, 32, dtype=torch.bfloat16, training=True, device=DEV)
+
+    def run():
+        out = [torch.empty_like(q) for _ in range(4)]
+        layer.forward(q, k, v, decay, out[0])
+        layer.backward(q, k, v, decay, do, *out[1:])
+        return out
+
+    clean = run()
+    q[T // 2, 0, 1, 5] = k[T // 2, 0, 1, 7] = v[T // 2, 0, 1, 9] = bad
+    for a, b in zip(clean, run()):
+        assert torch.equal(a[:, 1], b[:, 1]) and torch.equal(a[:, 0, 0], b[:, 0, 0]) and torch.equal(a[:, 0, 2], b[:, 0, 2])
+        assert torch.isnan(b[T // 2, 0, 1]).any() or torch.isinf(b[T // 2, 0, 1]).any()
+
+
+def test_two_captured_calls_at_the_same_time():
+    """Two graphs of the same layer (split along time: both use their workspaces) replayed on two streams side by side."""
+    cases = [Attention(2500, 1, 2, 1, 64, 64, "bf16", seed=s, decays=[-0.01, -1e-3]) for s in (1, 2)]
+    want, graphs = [], []
+    for c in cases:
+        c.forward()
+        c.backward()
+        torch.cuda.synchronize()
+        want.append({n: c.x[n].clone() for n in ("o", "dq", "dk", "dv")})
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.forward()
+            c.backward()
+        graphs.append(g)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for c in cases:
+            for n in want[0]:
+                c.x[n].zero_()
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for c, w in zip(cases, want):
+            assert all(torch.equal(c.x[n], w[n]) for n in w)
 
 
 def test_attention_binding_refuses_what_does_not_fit():
@@ -436,6 +518,28 @@ def test_dropout_offset_from_the_device_in_a_captured_call():
         torch.cuda.synchronize()
         want = torch.from_numpy(lo.dropout_factor(50, 72, 0.5, 4, 100 + i)).to(DEV).float()
         assert torch.equal(y, want) and torch.equal(z, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_beyond_32_bit_offsets(dtype):
+    """The same rows packed and 2^31 / 15 elements apart: the same bits."""
+    from paper_1503_02852_amd import layers
+    t, rows, dim, ld = TYPES[dtype], 17, 700, (1 << 31) // 15 // 8 * 8 + 8
+    r = np.random.default_rng(3)
+    big = torch.empty((rows - 1) * ld + 5 * 704, device=DEV, dtype=t)
+    far = [big[704 * i:].as_strided((rows, dim), (ld, 1)) for i in range(5)]
+    near = [rows_of(r, rows, dim, t) for _ in range(2)] + [torch.empty(rows, dim, device=DEV, dtype=t) for _ in range(3)]
+    for a, b in zip(far, near[:2]):
+        a.copy_(b)
+    layer = layers.AddNorm(rows, dim, dtype=t, dropout=0.3, seed=4, device=DEV)
+    rstd = torch.empty(rows, device=DEV)
+    gain = torch.from_numpy(r.standard_normal(dim).astype(np.float32)).to(DEV)
+    for x, res, h, y, z in (near, far):
+        layer.forward(x, y, residual=res, gain=gain, h=h, rstd=rstd)
+        layer.backward(y, h, rstd, gain=gain, dx=z, dresidual=res)
+        layers.dropout(z, x, 0.25, 7, 8)
+    for a, b in zip(far, near):
+        assert torch.equal(a, b)
 
 
 def test_block_of_layers_together():
