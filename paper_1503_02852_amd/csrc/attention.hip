@@ -617,7 +617,12 @@ struct ChunkShape { int DK, W, C, slices; };
 ChunkShape chunk_shape(int dtype, int dk, int dv) {
     ChunkShape s;
     s.DK = dk <= 64 ? 64 : dk <= 128 ? 128 : 256;
-    s.W = dv <= 64 ? 4 : 8;
+    // Columns of a workgroup: 64, or 128 (half as many reads of q and k, scores worked out once; fewer workgroups on a compute unit, which hide each
+    // other's waits less).  128 / 64 columns, us, 2,048 frames x 8 streams x 16 heads, forward and backward: bf16 128 x 128 units 124 / 125, 206 / 220,
+    // 256 x 256 232 / 242, 626 / 585; fp32 64 x 128 216 / 206, 673 / 609 (4,096 frames, one stream 250 / 289), 128 x 128 328 / 282, 806 / 626,
+    // 128 x 256 404 / 430, 256 x 256 750 / 843, 2217 / 2483.
+    const bool half = dv <= 64 || (dtype == DT_F32 ? s.DK == 128 && dv <= 128 : s.DK == 256);
+    s.W = half ? 4 : 8;
     s.C = chunk_frames(dtype == DT_F32, s.DK);
     s.slices = (dv + 16 * s.W - 1) / (16 * s.W);
     return s;
