@@ -16,11 +16,13 @@ __device__ __forceinline__ int length_of(const AttnCall& c, int n) { return c.le
 
 // ---------------------------------------------------------------------------------------------
 // Frame by frame.  A workgroup keeps 64 columns of one head's state in registers: 16 lanes of 4 columns, 16 of these side by side
-// with the rows r = lane group + 16 x.  For single frames it reads and writes the state once and is bound by that.
+// with the rows r = lane group + 16 x.  For single frames it reads and writes the state once and is bound by that: 192 streams x 16 heads x
+// 128 x 128 units 78 us (404 MB, 5.2 TB/s, as a copy).  Each further frame is a chain of its loads, sums over the rows and a barrier, 1.5 us.
 // ---------------------------------------------------------------------------------------------
 struct StepOps { AttnOp op[3]; };
 
-// WIDE: rows of the state whose quads of columns are whole and aligned.
+// WIDE: rows of the state whose quads of columns are whole and aligned, four numbers to a load (64 streams x 16 heads x 128 x 128, one frame, 26 us;
+// one number to a load, which transposed states need, 42).
 template <class T, int NR, bool WIDE>
 __global__ void __launch_bounds__(256) attention_steps_kernel(AttnCall c, StepOps ops, int slices) {
     const AttnOp& a = ops.op[blockIdx.y];
@@ -140,6 +142,12 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
+// Measured, 2,048 frames x 8 streams x 16 heads x 128 x 128 units, bf16: forward 136 us, backward 217 us (0.45 GB moved, 0.10 TFLOP: a third of the
+// memory's rate, a third of the matrix cores').  Without loads and stores backward takes 168 us, of which the state's update is 64 (as many vector
+// instructions for V' as matrix instructions), the state's part of the outputs 28, the scores 24, their product with V 25: a workgroup's phases follow
+// each other, and what a second one on the compute unit fills in is limited by the 384 workgroups there are for 256 compute units.  Half the LDS
+// reads (32 columns to a wavefront), keys a chunk ahead and one barrier fewer changed nothing; chunks of 32 frames take 220 us.
+// fp32: 607 us, 64 GFLOP at 0.75 of the fp32 matrix rate.
 struct ChunkOps {
     AttnOp op[3];
     float* seg_state[3];      // [segment][stream, head][dk][dv]: what a segment adds to the state, then the state before it
@@ -179,6 +187,8 @@ __device__ __forceinline__ bf16x8 split(f32x8& x) {
 }
 __device__ __forceinline__ bf16x8 rounded(f32x8 x) { return __builtin_convertvector(x, bf16x8); }
 
+// Frames of a chunk: as many as leave LDS room for two workgroups.  (bf16, 128 units, with 64 / 32: forward 136 / 142, backward 217 / 220, 4,096
+// frames of one stream 55.5 / 57.5, 16 streams forward 166 / 178 us.)
 constexpr int chunk_frames(bool f32, int DK) { return f32 || DK > 128 ? 32 : 64; }
 
 // Place of (frame, unit) of a tile of D units in LDS: the 16-byte pieces of a row are exchanged, so that neither 16 bytes of eight frames
@@ -194,7 +204,7 @@ __device__ __forceinline__ int place(int row, int col) {
 // weights and outputs are left out); what lies behind the units of a row stays zero from the start.  Rows have at least 16 bytes.
 // DIRECT (rows of whole 16-byte pieces, all aligned to them): straight to LDS, 64 lanes x 16 bytes at once in the order of the lanes, a lane
 // reading the piece that belongs in its place; s_waitcnt vmcnt(0) and a barrier make them visible.  Otherwise through registers, a row's last
-// 16 bytes from where they end.
+// 16 bytes from where they end.  (128 units, direct / through registers, us: bf16 forward 138 / 190, backward 218 / 342, fp32 backward 607 / 840.)
 template <class T, int C, int D, int THREADS, bool DIRECT>
 struct Tile {
     static constexpr int E = 16 / sizeof(T), ROW = D / E, ROWS = THREADS / ROW, PIECES = C / ROWS;      // pieces of a row; rows of a piece of all threads
@@ -601,7 +611,11 @@ static hipError_t launch_attention_steps(const AttnCall& c, const AttnOp* ops, i
     return c.dtype == DT_F32 ? go((float*)nullptr) : go((bf16_t*)nullptr);
 }
 
-// Segments of the frames, so that the chip is filled (two workgroups to a compute unit) where streams and heads are few.
+// Segments of the frames, so that the chip is filled (two workgroups to a compute unit) where streams and heads are few: each adds its frames up to a
+// state of its own, a scan makes these the states in front of the segments, and the outputs of all are worked out at once.  That reads k and v twice.
+// Whole / in segments, us, heads of 128 x 128 in bf16: 4,096 frames, 16 heads 260 / 55; 65,536 frames, 8 heads 4016 / 195; 2,048 frames x 8 streams x 16
+// heads forward (128 workgroups) 156 / 140; backward (384) 217 / 299: from 256 on they stay whole.  For 256, 512, 1,024 workgroups: 55, 55, 55; 240, 195, 208;
+// 150, 140, 171.  Segments of at least 2, 4, 8 chunks: 58, 55, 72 (4,096 frames).
 static int64_t most_segments(int T, int64_t works, int C) {      // (grows with T: room for a window's is room for a part's)
     const int64_t chunks = (T + C - 1) / C;
     return std::max<int64_t>(1, works >= 256 || works == 0 ? 1 : std::min<int64_t>((512 + works - 1) / works, chunks / 4));
