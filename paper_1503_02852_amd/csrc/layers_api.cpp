@@ -40,7 +40,8 @@ int check_workspace(const void* ws, int64_t have, int64_t need) {
 }
 
 // ---- rows ---------------------------------------------------------------------------------
-int check_rows(int64_t rows, int32_t dim, int32_t dtype, double p) {
+int check_rows(int64_t rows, int32_t dim, int32_t dtype, double p, const uint64_t* d_offset) {
+    if (misaligned(d_offset, 8)) return invalid("the offset's pointer is not aligned to its type");
     if (rows < 0 || rows > 2147483647) return invalid("rows must lie in [0, 2^31 - 1]");
     if (dim < 1) return invalid("dim must be positive");
     if (dtype < RNN_F32 || dtype > RNN_F16) return invalid("unknown dtype " + std::to_string(dtype));
@@ -55,7 +56,7 @@ int check_row_tensor(const char* name, const void* p, int64_t ld, int64_t rows, 
 }
 int check_norm(const rnn_add_norm_desc* d) {
     if (!d) return invalid("descriptor is NULL");
-    if (const int rc = check_rows(d->rows, d->dim, d->dtype, d->dropout)) return rc;
+    if (const int rc = check_rows(d->rows, d->dim, d->dtype, d->dropout, d->d_offset)) return rc;
     if (d->dim > NORM_MAX_DIM) return invalid("norm: dim exceeds " + std::to_string(NORM_MAX_DIM));
     if (!(d->eps >= 0.0f) || std::isinf(d->eps)) return invalid("norm: eps must be finite and not negative");
     return RNN_OK;
@@ -183,6 +184,8 @@ int rnn_linear_attention_forward(const rnn_linear_attention_desc* d, const rnn_f
         if (!rc) rc = check_floats("state_in", d_state_in);
         if (!rc) rc = check_floats("state_out", d_state_out);
         if (!rc && !d_log_decay) rc = invalid("attention: log_decay pointer is NULL");
+        if (!rc) rc = check_floats("log_decay", d_log_decay);
+        if (!rc) rc = check_floats("lengths", d_lengths);
         if (!rc && !with_o && !d_state_out) rc = invalid("attention: neither o nor state_out is given");
         const AttnSpace w = space_of(d, false);
         if (!rc) rc = check_workspace(d_workspace, ws_bytes, w.total);
@@ -212,6 +215,8 @@ int rnn_linear_attention_backward(const rnn_linear_attention_desc* d, const rnn_
         if (!rc) rc = check_floats("dstate_out", d_dstate_out);
         if (!rc) rc = check_floats("dstate_in", d_dstate_in);
         if (!rc && !d_log_decay) rc = invalid("attention: log_decay pointer is NULL");
+        if (!rc) rc = check_floats("log_decay", d_log_decay);
+        if (!rc) rc = check_floats("lengths", d_lengths);
         if (!rc && d_dstate_in && d_dstate_in == d_dstate_out) rc = invalid("attention: dstate_in may not be dstate_out");
         const AttnSpace w = space_of(d, true);
         if (!rc) rc = check_workspace(d_workspace, ws_bytes, w.total);
@@ -293,7 +298,7 @@ int rnn_add_norm_backward(const rnn_add_norm_desc* d, const void* d_dy, int64_t 
 int rnn_dropout(const rnn_dropout_desc* d, const void* d_x, int64_t ld_x, void* d_y, int64_t ld_y, void* hip_stream) {
     return guarded([&]() -> int {
         if (!d) return invalid("descriptor is NULL");
-        if (const int rc = check_rows(d->rows, d->dim, d->dtype, d->p)) return rc;
+        if (const int rc = check_rows(d->rows, d->dim, d->dtype, d->p, d->d_offset)) return rc;
         const int b = size_of(d->dtype);
         int rc = check_row_tensor("x", d_x, ld_x, d->rows, d->dim, b, true);
         if (!rc) rc = check_row_tensor("y", d_y, ld_y, d->rows, d->dim, b, true);

@@ -225,3 +225,47 @@ def test_character_model():
     for a, b in zip(gw + gb, ref["grad_w"] + ref["grad_b"]):
         if b is not None:
             assert nerr(a, b) < GRAD_TOL
+
+
+def test_class_indices_straight_into_the_layers():
+    """One-hot inputs given as class indices whose connections lead into norm and attention nodes, one of them delayed."""
+    g = wl.GraphSpec()
+    x = g.add_node(wl.INPUT, wl.LINEAR, 9, name="x")
+    n = g.add_node(wl.NORM, wl.LINEAR, 32, has_bias=True, name="norm")
+    g.add_edge(x, n, wl.FULL)
+    g.add_edge(x, n, wl.FULL, 2)
+    a = g.add_node(wl.ATTENTION, wl.LINEAR, 32, name="att", heads=2, scale=0.3, log_decay=np.array([-0.05, -0.5]))
+    g.add_edge(x, a, wl.FULL)
+    g.add_edge(n, a, wl.IDENTITY)
+    g.add_edge(x, a, wl.FULL, 1)
+    out = g.add_node(wl.ADD, wl.SOFTMAX, 5, has_bias=True, is_output=1, name="out")
+    g.add_edge(a, out, wl.FULL)
+    g.add_edge(n, out, wl.FULL)
+    T, N = 37, 3
+    w = wl.make_workload("classes", g, T, N, seed=6, scale=0.5)
+    idx = np.random.default_rng(8).integers(-1, 9, size=(T, N))
+    w.inputs[x] = np.where(idx[..., None] >= 0, np.eye(9, dtype=np.float32)[idx], 0).astype(np.float32)
+    win = window_of(w, T)
+    win.set_onehot_inputs({x: idx})
+    win.step()
+    compare(win, go.forward_bptt(g.nodes, g.edges, w.weights, w.biases, w.inputs, w.targets, T, N), g, "classes")
+
+
+def test_layers_between_recurrent_layers():
+    """LSTM -> norm -> LSTM -> attention: the recurrent layers run as their step kernels, the layers between their launches."""
+    g = wl.GraphSpec()
+    x = g.add_node(wl.INPUT, wl.LINEAR, 12, name="x")
+    h = wl.add_lstm_layer(g, x, 32, "L1")["h"]
+    n = g.add_node(wl.NORM, wl.LINEAR, 32, has_bias=True, name="norm")
+    g.add_edge(h, n, wl.IDENTITY)
+    d = g.add_node(wl.DROPOUT, wl.LINEAR, 32, name="drop", dropout=(0.2, 11, 3))
+    g.add_edge(n, d, wl.IDENTITY)
+    h2 = wl.add_lstm_layer(g, d, 32, "L2")["h"]
+    a = g.add_node(wl.ATTENTION, wl.LINEAR, 32, name="att", heads=4, scale=0.35, log_decay=-np.array([0.0, 0.1, 0.01, 1.0]))
+    for _ in range(3):
+        g.add_edge(h2, a, wl.FULL)
+    out = g.add_node(wl.ADD, wl.SOFTMAX, 5, has_bias=True, is_output=1, name="out")
+    g.add_edge(a, out, wl.FULL)
+    g.add_edge(h2, out, wl.FULL)
+    for N in (1, 20):
+        run_both(wl.make_workload("stack", g, 50, N, seed=N, scale=0.3), label=f"stack N={N}")

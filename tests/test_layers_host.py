@@ -129,3 +129,17 @@ def test_row_argument_refusals():
     refused(lib.rnn_dropout(drop(), None, 40, P, 40, None), "x pointer")
     refused(lib.rnn_dropout(drop(), P, 40, P, 39, None), "y: ld")
     assert lib.rnn_dropout(drop(rows=0), None, 40, None, 40, None) == 0
+
+
+def test_misaligned_vectors_are_refused():
+    """Scalar loads drop an address's low bits: another element would be read."""
+    lib = load_library()
+    f = frames()
+    for p in (P + 1, P + 2):
+        refused(lib.rnn_linear_attention_forward(attention(), f, f, f, p, None, None, None, f, None, 0, None), "log_decay")
+        refused(lib.rnn_linear_attention_forward(attention(), f, f, f, P, p, None, None, f, None, 0, None), "lengths")
+        refused(lib.rnn_linear_attention_backward(attention(), f, f, f, p, None, None, f, None, f, f, f, None, P, 1 << 30, None), "log_decay")
+        refused(lib.rnn_linear_attention_backward(attention(), f, f, f, P, p, None, f, None, f, f, f, None, P, 1 << 30, None), "lengths")
+    for p in (P + 1, P + 4):
+        refused(lib.rnn_dropout(drop(d_offset=p), P, 40, P, 40, None), "offset")
+        refused(lib.rnn_add_norm_forward(norm(dropout=0.5, d_offset=p), P, 40, None, 0, None, None, 0, P, 40, None, None), "offset")
