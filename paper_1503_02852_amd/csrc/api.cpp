@@ -1348,7 +1348,7 @@ int run_attention(rnn_graph* g, int i, const float* from, float* to, int t0, int
     const LayerPlan& lp = P.layers[i];
     const rnn_linear_attention_desc d = g->attention_desc(i, t1 - t0, g->N);
     rnn_frames x[3], o = layer_heads(g, P.ybuf(lp.node), t0, d.heads);
-    for (int j = 0; j < 3; ++j) x[j] = layer_heads(g, P.ybuf(lp.sums[j]), t0, d.heads);
+    for (int j = 0; j < 3; ++j) x[j] = layer_heads(g, lp.reads[j], t0, d.heads);
     return rnn_linear_attention_forward(&d, &x[0], &x[1], &x[2], g->layer_settings[i].d_log_decay, nullptr, from, to, with_outputs ? &o : nullptr,
                                         layer_scratch(g), rnn_linear_attention_workspace_bytes(&d, 0), s);
 }
@@ -1373,12 +1373,12 @@ int layer_forward(rnn_graph* g, int i, int t0, int t1, hipStream_t s) {
     } else if (lp.kind == NODE_NORM) {
         AddNormArgs a = {};
         a.rows = (int64_t)(t1 - t0) * g->N; a.dim = P.xnodes[lp.node].dim; a.eps = RNN_NORM_EPS;
-        a.x = layer_rows(g, P.ybuf(lp.sums[0]), t0); a.y = layer_rows(g, P.ybuf(lp.node), t0);
+        a.x = layer_rows(g, lp.reads[0], t0); a.y = layer_rows(g, P.ybuf(lp.node), t0);
         a.gain = P.nodes[lp.node].has_bias ? g->weights + P.bias_off[lp.node] : nullptr;
         a.rstd = static_cast<float*>(layer_rows(g, P.abuf(lp.node), t0).p);
         e = launch_add_norm(DT_F32, a, s);
     } else {
-        e = launch_dropout(DT_F32, layer_dropout(g, i, P.ybuf(lp.sums[0]), P.ybuf(lp.node), t0, t1), s);
+        e = launch_dropout(DT_F32, layer_dropout(g, i, lp.reads[0], P.ybuf(lp.node), t0, t1), s);
     }
     g->prof.end(prof, 1, s);
     return e == hipSuccess ? RNN_OK : fail_hip(e, "layer");
@@ -1388,7 +1388,7 @@ AddNormGradArgs norm_grad_args(rnn_graph* g, int i, int t0, int t1) {
     const LayerPlan& lp = P.layers[i];
     AddNormGradArgs a = {};
     a.rows = (int64_t)(t1 - t0) * g->N; a.dim = P.xnodes[lp.node].dim;
-    a.dy = layer_rows(g, P.dbuf(lp.node), t0); a.h = layer_rows(g, P.ybuf(lp.sums[0]), t0);
+    a.dy = layer_rows(g, P.dbuf(lp.node), t0); a.h = layer_rows(g, lp.reads[0], t0);
     a.gain = P.nodes[lp.node].has_bias ? g->weights + P.bias_off[lp.node] : nullptr;
     a.rstd = static_cast<float*>(layer_rows(g, P.abuf(lp.node), t0).p);
     a.blocks = norm_grad_blocks(a.rows, a.dim);
@@ -1403,7 +1403,7 @@ int layer_backward(rnn_graph* g, int i, int t0, int t1, hipStream_t s) {
     if (lp.kind == NODE_ATTENTION) {
         const rnn_linear_attention_desc d = g->attention_desc(i, t1 - t0, g->N);
         rnn_frames x[3], dx[3], d_o = layer_heads(g, P.dbuf(lp.node), t0, d.heads);
-        for (int j = 0; j < 3; ++j) { x[j] = layer_heads(g, P.ybuf(lp.sums[j]), t0, d.heads); dx[j] = layer_heads(g, P.dbuf(lp.sums[j]), t0, d.heads); }
+        for (int j = 0; j < 3; ++j) { x[j] = layer_heads(g, lp.reads[j], t0, d.heads); dx[j] = layer_heads(g, P.dbuf(lp.sums[j]), t0, d.heads); }
         const int rc = rnn_linear_attention_backward(&d, &x[0], &x[1], &x[2], g->layer_settings[i].d_log_decay, nullptr,
                                                      reinterpret_cast<float*>(g->ws + g->layout.state_off[i]), &d_o, nullptr, &dx[0], &dx[1], &dx[2], nullptr,
                                                      layer_scratch(g), rnn_linear_attention_workspace_bytes(&d, 1), s);

@@ -333,7 +333,7 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
     for (int k = 0; k < K0; ++k)
         if (whole_frames(nodes[k].kind)) {
             layer_of[k] = (int)P.layers.size();
-            LayerPlan lp{nodes[k].kind, k, {-1, -1, -1}};
+            LayerPlan lp{nodes[k].kind, k, {-1, -1, -1}, {-1, -1, -1}};
             const int n_sums = nodes[k].kind == NODE_ATTENTION ? 3 : 1;
             for (int i = 0; i < n_sums; ++i) {
                 lp.sums[i] = (int)P.xnodes.size();
@@ -378,9 +378,19 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
         if (xn[k].kind != NODE_INPUT) P.buf_alloc[P.ybuf(k)] = P.buf_alloc[P.dbuf(k)] = 1;
         else if (P.input_staged[k]) P.buf_alloc[P.ybuf(k)] = 1;
     }
-    std::vector<char> sum_of_layer(K, 0);
-    for (const LayerPlan& lp : P.layers) {
-        for (int s : lp.sums) if (s >= 0) sum_of_layer[s] = 1;
+    std::vector<char> sum_of_layer(K, 0);      // 2: one that is not computed
+    std::vector<int> n_into(K, 0), last_into(K, -1);
+    for (int m = 0; m < M; ++m) { ++n_into[xe[m].dst]; last_into[xe[m].dst] = m; }
+    for (LayerPlan& lp : P.layers) {
+        for (int i = 0; i < 3; ++i) {
+            const int s = lp.sums[i];
+            if (s < 0) continue;
+            const GEdge& e = xe[last_into[s]];
+            const bool same = n_into[s] == 1 && e.wkind == W_IDENTITY && e.delay == 0;
+            sum_of_layer[s] = same ? 2 : 1;
+            lp.reads[i] = P.ybuf(same ? e.src : s);
+            if (same) P.buf_alloc[P.ybuf(s)] = 0;
+        }
         if (lp.kind == NODE_NORM) { P.buf_dim[P.abuf(lp.node)] = 1; P.buf_alloc[P.abuf(lp.node)] = 1; }
     }
     // y_src of a full connection inside a recurrent node is read by all workgroups during the
@@ -434,7 +444,8 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
             if (xn[k].act == ACT_SOFTMAX) cp.softmax_node = k;
             else if (xn[k].is_output == OUT_SQUARED_ERROR) cp.sqerr_node = k;
         }
-        for (int p = 0; p < (cp.layer >= 0 ? 0 : n_phases); ++p) {      // (a layer's forward pass is its kernel's alone)
+        const bool program = cp.layer < 0 && sum_of_layer[members[0]] != 2;      // (a layer's forward pass is its kernel's alone)
+        for (int p = 0; p < (program ? n_phases : 0); ++p) {
             std::vector<int> np;
             for (int k : members) if (phase[k] == p) np.push_back(k);
             std::map<int, int> slot;
@@ -494,7 +505,7 @@ bool build_plan(const std::vector<GNode>& nodes, const std::vector<GEdge>& edges
             for (int k : members) if (shared_y[k]) shared[P.ybuf(k)] = 1;
             if (!emit_phase(P, cp.fwd_phases, tasks, ops, part_bufs, written, shared, cp.recurrent ? -1 : 0, err)) return false;
         }
-        cp.has_fwd_program = cp.layer < 0;
+        cp.has_fwd_program = program;
         if (!cp.recurrent && members.size() == 1 && xn[members[0]].kind == NODE_ADD && cp.fwd_gemms.size() == 1) {
             const int k = members[0];
             cp.in_products = cp.fwd_gemms[0].c_buf == P.ybuf(k);

@@ -63,8 +63,10 @@ struct CompPlan {
 };
 
 // A norm, attention or dropout node.  Its connections lead into linear additive nodes of the execution graph, one for all of them or (attention)
-// one for each, whose activations its kernel reads and whose error terms it writes.  Norm: 1 / root mean square per row is kept in abuf(node).
-struct LayerPlan { int kind, node, sums[3]; };
+// one for each, whose error terms its kernel writes.  It reads their activations (`reads`: buffer ids) or, where such a sum is a single undelayed
+// identity connection, those of that connection's source: the sum is then not computed and has no tensor.  Norm: 1 / root mean square per row is
+// kept in abuf(node).
+struct LayerPlan { int kind, node, sums[3], reads[3]; };
 
 // Consecutive recurrent components first..last whose step loops can run side by side in one
 // kernel launch: members[i] is component first + i lowered with the full connections between
