@@ -269,3 +269,35 @@ def test_layers_between_recurrent_layers():
     g.add_edge(h2, out, wl.FULL)
     for N in (1, 20):
         run_both(wl.make_workload("stack", g, 50, N, seed=N, scale=0.3), label=f"stack N={N}")
+
+
+def test_layers_read_in_place():
+    """Layers on a lone identity connection: of an input, of another layer, of a recurrent layer; all three of attention's from one node.  The
+    window moves on, so that the copies of inputs and the layers' tensors are shifted."""
+    g = wl.GraphSpec()
+    x = g.add_node(wl.INPUT, wl.LINEAR, 24, name="x")
+    n = g.add_node(wl.NORM, wl.LINEAR, 24, name="norm")
+    g.add_edge(x, n, wl.IDENTITY)
+    d = g.add_node(wl.DROPOUT, wl.LINEAR, 24, name="drop", dropout=(0.4, 2, 0))
+    g.add_edge(n, d, wl.IDENTITY)
+    a = g.add_node(wl.ATTENTION, wl.LINEAR, 24, name="att", heads=3, scale=0.3, log_decay=np.array([-0.3, -0.02, 0.0]))
+    for _ in range(3):
+        g.add_edge(d, a, wl.IDENTITY)
+    h = wl.add_lstm_layer(g, a, 24, "L")["h"]
+    n2 = g.add_node(wl.NORM, wl.LINEAR, 24, has_bias=True, name="norm2")
+    g.add_edge(h, n2, wl.IDENTITY)
+    out = g.add_node(wl.ADD, wl.SOFTMAX, 5, has_bias=True, is_output=1, name="out")
+    g.add_edge(n2, out, wl.FULL)
+    g.add_edge(n, out, wl.FULL, 3)
+    T, step, N = 20, 7, 3
+    w = wl.make_workload("in place", g, T + 2 * step, N, seed=12, scale=0.3)
+    y, z = go.forward(g.nodes, g.edges, w.weights, w.biases, w.inputs, T + 2 * step, N)
+    win = window_of(w, T)
+    win.forward()
+    for i in range(3):
+        if i:
+            cut = slice(T + (i - 1) * step, T + i * step)
+            win.advance({k: v[cut] for k, v in w.inputs.items()}, {k: v[cut] for k, v in w.targets.items()})
+        win.bptt()
+        win.compute_grads()
+        compare(win, go.bptt_window(g.nodes, g.edges, w.weights, w.biases, y, z, w.targets, i * step, T, N), g, f"in place {i}")
