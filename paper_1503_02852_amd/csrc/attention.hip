@@ -133,8 +133,8 @@ __global__ void __launch_bounds__(256) attention_steps_kernel(AttnCall c, StepOp
 // fp32 takes the matrix cores' fp32 products.  bf16 takes its inputs as they are; of what is computed, the scores and the state that outputs are
 // made from are rounded to bf16.  Their errors, 2^-9 of a term at most and independent of each other, add up like the roundings of the results
 // themselves: a result's error is at most 1.41 times what its own rounding leaves.  (In two parts of 8 bits each it would not grow, at 20 % more
-// time.)  The state that is carried on is another matter: V' is split into two bf16 numbers, which lose 2^-17 of it, and into three, which keep all
-// of its bits, where the last state is asked for.
+// time.)  The state that is carried on is another matter: V' is split into three bf16 numbers, which keep all of its bits, whether the last state is
+// asked for or not.
 // ---------------------------------------------------------------------------------------------
 typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
 typedef bf16_t bf16x4 __attribute__((ext_vector_type(4)));
@@ -152,7 +152,6 @@ struct ChunkOps {
     AttnOp op[3];
     float* seg_state[3];      // [segment][stream, head][dk][dv]: what a segment adds to the state, then the state before it
     int n_ops, slices, n_seg, seg_len;
-    bool whole_state;         // some operator's last state is asked for
     unsigned works;
 };
 
@@ -291,7 +290,6 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), g = lane / 16, m = lane % 16;
     const int my_col = col0 + 16 * wave + m, out_col = col0 + 16 * wave + 4 * g;      // the lane's column; the first of the four it has of an output
     const bool busy = col0 + 16 * wave < a.dv;                                        // of a wavefront; the others help with the tiles and scores
-    const bool whole_state = STATE ? ops.whole_state : a.s_out != nullptr;            // three parts of V'
 
     TileK tq(a.q, n, h, 0, a.dk, a.reverse, L, begin), tk(a.k, n, h, 0, a.dk, a.reverse, L, begin);
     TileV tv(a.v, n, h, col0, a.dv, a.reverse, L, begin);
@@ -502,9 +500,7 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
                     f32x8 x = __builtin_convertvector(v_frames(s), f32x8);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] *= wt[32 * s + 8 * g + e];
-                    bf16x8 v0 = split(x), v1, v2;
-                    if (whole_state) { v1 = split(x); v2 = rounded(x); }
-                    else v1 = v2 = rounded(x);
+                    const bf16x8 v0 = split(x), v1 = split(x), v2 = rounded(x);
 #pragma unroll
                     for (int t = 0; t < AT; t += 2) {
                         const bf16x8 k[2] = {k_frames(s, t), k_frames(s, t + 1)};
@@ -512,9 +508,8 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
                         for (int u = 0; u < 2; ++u) S[t + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u], v0, S[t + u], 0, 0, 0);
 #pragma unroll
                         for (int u = 0; u < 2; ++u) S[t + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u], v1, S[t + u], 0, 0, 0);
-                        if (whole_state)
 #pragma unroll
-                            for (int u = 0; u < 2; ++u) S[t + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u], v2, S[t + u], 0, 0, 0);
+                        for (int u = 0; u < 2; ++u) S[t + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u], v2, S[t + u], 0, 0, 0);
                     }
                 }
             }
@@ -665,7 +660,6 @@ hipError_t launch_attention(const AttnCall& c, const AttnOp* ops, int n_ops, flo
     for (int i = 0; i < n_ops; ++i) {
         const AttnOp& a = co.op[i] = ops[i];
         dk = std::max(dk, a.dk); dv = std::max(dv, a.dv);
-        co.whole_state = co.whole_state || a.s_out;
         direct = direct && a.dk % E == 0 && a.dv % E == 0;
         for (const AttnTensor* x : {&a.q, &a.k, &a.v})
             direct = direct && reinterpret_cast<uintptr_t>(x->p) % 16 == 0 && x->st % E == 0 && x->sn % E == 0 && x->sh % E == 0;
