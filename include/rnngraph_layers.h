@@ -19,8 +19,8 @@
  *    not share a place.  Alignment: that of the element type.
  *  - Sums, statistics and states are fp32 whatever the type of the tensors, and what is stored is rounded once, to
  *    nearest.  Attention on RNN_BF16 tensors multiplies with the matrix instructions for bf16: the scores between frames of
- *    a chunk and, for outputs and gradients, the state that the chunk starts from are rounded to bf16 as their
- *    operands (the state that is handed on is not).
+ *    a chunk and, for outputs and gradients, the state that the chunk starts from go there in two bf16 numbers each, which
+ *    lose at most 2^-16 of a term of the result's sum (the state that is handed on loses nothing by it).
  */
 #ifndef RNNGRAPH_LAYERS_H
 #define RNNGRAPH_LAYERS_H

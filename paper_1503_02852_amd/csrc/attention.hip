@@ -130,11 +130,12 @@ __global__ void __launch_bounds__(256) attention_steps_kernel(AttnCall c, StepOp
 // product's first operand over those rows: the state never leaves the registers.  The operands that run along frames (V, K^T) come out of
 // LDS through the transposing read, which takes columns in fours from anywhere: state tiles 2 t and 2 t + 1 have the rows of which a lane
 // reads eight neighbouring ones of q.
-// fp32 takes the matrix cores' fp32 products.  bf16 takes its inputs as they are; of what is computed, the scores and the state that outputs are
-// made from are rounded to bf16.  Their errors, 2^-9 of a term at most and independent of each other, add up like the roundings of the results
-// themselves: a result's error is at most 1.41 times what its own rounding leaves.  (In two parts of 8 bits each it would not grow, at 20 % more
-// time.)  The state that is carried on is another matter: V' is split into three bf16 numbers, which keep all of its bits, whether the last state is
-// asked for or not.
+// fp32 takes the matrix cores' fp32 products.  bf16 takes its inputs as they are; what is computed goes to the matrix cores in several bf16 numbers
+// whose sum it is.  V' in three, which keep all of its bits: the state is carried on in 32 bits, whether it is asked for or not.  Scores, and the
+// state as an operand of the outputs, in OPERAND_PARTS = 2: 2^-16 of a term is lost at most (the upper eight bits are cut off, the rest is rounded to
+// eight), which is what 256 of the fp32 additions that make a result (some 4 (dk + dv) + 8 a frame between) may take.  In one number 2^-9 of a term
+// would be lost, which results whose terms cancel (keys and values around one, queries that sum up to nothing) do not stand.  In one / two / three,
+// us, 2,048 frames x 8 streams x 16 heads x 128 x 128, forward and backward: 136, 227 / 141, 253 / 151, 282; 65,536 frames, 8 heads: 194 / 209 / 226.
 // ---------------------------------------------------------------------------------------------
 typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
 typedef bf16_t bf16x4 __attribute__((ext_vector_type(4)));
@@ -174,17 +175,24 @@ __device__ __forceinline__ unsigned upper(float& x, float& y) {
     y -= __builtin_bit_cast(float, b & 0xFFFF0000u);
     return __builtin_amdgcn_perm(b, a, 0x07060302u);
 }
-__device__ __forceinline__ bf16x8 split(f32x8& x) {
-    union { unsigned u[4]; bf16x8 v; } r;
+// Numbers in fp32 as the sum of N in bf16: eight of the 24 bits each, with three of them all.
+constexpr int OPERAND_PARTS = 2;
+template <int N, class F, class B>
+__device__ __forceinline__ void split(F x, B (&part)[N]) {
+    constexpr int PAIRS = sizeof(F) / 8;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float a = x[2 * i], b = x[2 * i + 1];
-        r.u[i] = upper(a, b);
-        x[2 * i] = a; x[2 * i + 1] = b;
+    for (int p = 0; p < N - 1; ++p) {
+        union { unsigned u[PAIRS]; B v; } r;
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            float a = x[2 * i], b = x[2 * i + 1];
+            r.u[i] = upper(a, b);
+            x[2 * i] = a; x[2 * i + 1] = b;
+        }
+        part[p] = r.v;
     }
-    return r.v;
+    part[N - 1] = __builtin_convertvector(x, B);
 }
-__device__ __forceinline__ bf16x8 rounded(f32x8 x) { return __builtin_convertvector(x, bf16x8); }
 
 // Frames of a chunk: as many as leave LDS room for two workgroups.  (bf16, 128 units, with 64 / 32: forward 136 / 142, backward 217 / 220, 4,096
 // frames of one stream 55.5 / 57.5, 16 streams forward 166 / 178 us.)
@@ -266,7 +274,7 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
     constexpr int BUFS = STATE ? 2 : 1;                                               // (the state alone: no room is needed for q and the scores)
     __shared__ alignas(256) T lds_ks[BUFS * C * DK];
     __shared__ alignas(256) T lds_vs[BUFS * C * BV];
-    __shared__ alignas(256) T lds_p[STATE ? 8 : F32 ? C * (C + 4) : C * C];           // scores [i][j]
+    __shared__ alignas(256) T lds_p[STATE ? 8 : F32 ? C * (C + 4) : OPERAND_PARTS * C * C];       // scores [i][j]; bf16: their parts one behind the other
     __shared__ float chunk_decay;
     __shared__ double exact_decay, carry;                                             // g^C; what the roundings of chunk_decay have left so far: the next makes up for it
     __shared__ float power[16 + C + 1], weight[2 * C];                                // g^i from 16 on (what is before it goes to masked scores only); update g^(C - j - early), zeros
@@ -304,7 +312,7 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
         tk.load(lds_ks, end - begin);
         tv.load(lds_vs, end - begin);
     }
-    if constexpr (!STATE) clear_lds(lds_p, F32 ? C * (C + 4) : C * C);                // (tiles above the diagonal stay zero)
+    if constexpr (!STATE) clear_lds(lds_p, F32 ? C * (C + 4) : OPERAND_PARTS * C * C);                // (tiles above the diagonal stay zero)
     const float ld = log_decay_of(c, h), both = a.out * a.update;
     if (threadIdx.x <= C + 16) power[threadIdx.x] = threadIdx.x < 16 ? 0.0f : (float)exp((double)ld * ((int)threadIdx.x - 16));
     if (threadIdx.x == C) { exact_decay = exp((double)ld * C); carry = 1.0; }
@@ -383,9 +391,12 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
 #pragma unroll
                     for (int it = 0; it < IT; ++it) qf[it] = along(lds_q, it, t);
                     const f32x8 s = __builtin_shufflevector(S[2 * t], S[2 * t + 1], 0, 1, 2, 3, 4, 5, 6, 7);
-                    const bf16x8 sf = rounded(s);
+                    bf16x8 sf[OPERAND_PARTS];
+                    split(s, sf);
 #pragma unroll
-                    for (int it = 0; it < IT; ++it) acc[it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sf, qf[it], acc[it], 0, 0, 0);
+                    for (int u = 0; u < OPERAND_PARTS; ++u)
+#pragma unroll
+                        for (int it = 0; it < IT; ++it) acc[it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sf[u], qf[it], acc[it], 0, 0, 0);
                 }
             }
 #pragma unroll
@@ -426,7 +437,12 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
                 for (int r = 0; r < 4; ++r) s[r] = (lag >= r ? s[r] : 0.0f) * (both * f[-r]);
                 T* p = lds_p + score_at(16 * it + m, 16 * jt + 4 * g);
                 if constexpr (F32) *(f32x4*)p = s;
-                else *(bf16x4*)p = __builtin_convertvector(s, bf16x4);
+                else {
+                    bf16x4 part[OPERAND_PARTS];
+                    split(s, part);
+#pragma unroll
+                    for (int u = 0; u < OPERAND_PARTS; ++u) *(bf16x4*)(p + u * C * C) = part[u];
+                }
             }
             __syncthreads();                   // the scores are there, q has been read
             if (first + C < end) tq.load(lds_q, end - first - C);
@@ -449,11 +465,14 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
 #pragma unroll
                     for (int s = 0; s < C / 32; ++s) {
                         const bf16x8 v = v_frames(s);
-                        bf16x8 pf[IT];
 #pragma unroll
-                        for (int it = 2 * s; it < IT; ++it) pf[it] = *(const bf16x8*)(lds_p + score_at(16 * it + m, 32 * s + 8 * g));
+                        for (int u = 0; u < OPERAND_PARTS; ++u) {
+                            bf16x8 pf[IT];
 #pragma unroll
-                        for (int it = 2 * s; it < IT; ++it) acc[it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[it], acc[it], 0, 0, 0);
+                            for (int it = 2 * s; it < IT; ++it) pf[it] = *(const bf16x8*)(lds_p + u * C * C + score_at(16 * it + m, 32 * s + 8 * g));
+#pragma unroll
+                            for (int it = 2 * s; it < IT; ++it) acc[it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[it], acc[it], 0, 0, 0);
+                        }
                     }
                 }
                 const int64_t step = a.reverse ? -a.o.st : a.o.st;
@@ -500,16 +519,15 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
                     f32x8 x = __builtin_convertvector(v_frames(s), f32x8);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] *= wt[32 * s + 8 * g + e];
-                    const bf16x8 v0 = split(x), v1 = split(x), v2 = rounded(x);
+                    bf16x8 v[3];
+                    split(x, v);
 #pragma unroll
                     for (int t = 0; t < AT; t += 2) {
                         const bf16x8 k[2] = {k_frames(s, t), k_frames(s, t + 1)};
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) S[t + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u], v0, S[t + u], 0, 0, 0);
+                        for (int p = 0; p < 3; ++p)
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) S[t + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u], v1, S[t + u], 0, 0, 0);
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) S[t + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u], v2, S[t + u], 0, 0, 0);
+                            for (int u = 0; u < 2; ++u) S[t + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u], v[p], S[t + u], 0, 0, 0);
                     }
                 }
             }
