@@ -181,7 +181,7 @@ int rnn_set_onehot_input(rnn_graph* g, int32_t input, const int32_t* d_indices);
 
 /* Heads of an attention node (they divide its units into heads of at most 256), the factor of its
  * outputs, and d_log_decay, DEVICE float [heads], each at most 0 (0: nothing is forgotten, -inf:
- * everything; positive values count as 0), which must stay valid and unchanged while windows run; it
+ * everything; positive values count as 0, NaN gives NaN), which must stay valid and unchanged while windows run; it
  * has no gradient.  Needed before rnn_workspace_bytes and the first window (RNN_ERR_SEQUENCE); ends the
  * current window. */
 int rnn_set_attention(rnn_graph* g, int32_t node, int32_t heads, float scale, const float* d_log_decay);

@@ -47,7 +47,7 @@ enum rnn_dtype { RNN_F32 = 0, RNN_BF16 = 1, RNN_F16 = 2 };
  *   dim_k, dim_v  1 .. 256 units of a head
  *   dtype       of q, k, v, o and their gradients: RNN_F32 or RNN_BF16
  * d_log_decay: float [heads], at most 0 (0: nothing is forgotten, -inf: everything; positive values
- * count as 0).  It has no gradient: the decays are constants of the layer.
+ * count as 0; a head whose decay is NaN has NaN wherever its state has passed a frame).  It has no gradient: the decays are constants of the layer.
  * d_lengths: int32 [N] or NULL.  Stream n has its first d_lengths[n] frames (values outside [0, T]
  * count as the nearer end); what lies behind them is not read, outputs there stay as they were.
  * d_state_in: float [N][heads][dim_k][dim_v] or NULL (zero).  d_state_out: the state after the

@@ -9,9 +9,12 @@ namespace {
 typedef __bf16 bf16_t;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// 0 >= log decay; a positive one counts as 0 (and so does NaN).  exp is 0 from about -104 on, so the bound below changes no value, and
+// 0 >= log decay; a positive one counts as 0, NaN stays.  exp is 0 from about -104 on, so the bound below changes no value, and
 // 0 times it is 0 (0 times -inf is not).
-__device__ __forceinline__ float log_decay_of(const AttnCall& c, int h) { return fmaxf(fminf(c.log_decay[h], 0.0f), -1000.0f); }
+__device__ __forceinline__ float log_decay_of(const AttnCall& c, int h) {
+    const float x = c.log_decay[h];
+    return x != x ? x : fmaxf(fminf(x, 0.0f), -1000.0f);
+}
 __device__ __forceinline__ int length_of(const AttnCall& c, int n) { return c.lengths ? min(max(c.lengths[n], 0), c.T) : c.T; }
 
 // ---------------------------------------------------------------------------------------------
@@ -314,7 +317,7 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
     }
     if constexpr (!STATE) clear_lds(lds_p, F32 ? C * (C + 4) : OPERAND_PARTS * C * C);                // (tiles above the diagonal stay zero)
     const float ld = log_decay_of(c, h), both = a.out * a.update;
-    if (threadIdx.x <= C + 16) power[threadIdx.x] = threadIdx.x < 16 ? 0.0f : (float)exp((double)ld * ((int)threadIdx.x - 16));
+    if (threadIdx.x <= C + 16) power[threadIdx.x] = threadIdx.x < 16 ? 0.0f : threadIdx.x == 16 ? 1.0f : (float)exp((double)ld * ((int)threadIdx.x - 16));
     if (threadIdx.x == C) { exact_decay = exp((double)ld * C); carry = 1.0; }
     if (threadIdx.x < 2 * C) weight[threadIdx.x] = threadIdx.x < C ? a.update * expf(ld * (C - (int)threadIdx.x - (a.early ? 1 : 0))) : 0.0f;
 
