@@ -39,8 +39,8 @@ enum rnn_dtype { RNN_F32 = 0, RNN_BF16 = 1, RNN_F16 = 2 };
  * that is o(t) = scale sum_{s <= t} exp((t - s) log_decay[h]) (q(t) . k(s)) v(s) + the part of
  * the state before the window.  Frames are worked on together, in chunks (Section 3.1's aim for
  * a recurrence that has no nonlinearity); few frames (up to 4) one after another.  An infinity or NaN in a
- * frame makes outputs of earlier frames of its chunk (up to 63 back) NaN as well as later ones (gradients
- * likewise, backwards in time); those of other streams and heads never.
+ * frame reaches what the formulas make of that frame, where an infinity may become NaN: outputs and dq of it
+ * and later frames, dk and dv of it and earlier ones, of its stream and head.
  *   T, N        frames and streams; T = 0 and N = 0 are allowed
  *   heads       heads of q and o; kv_heads heads of k and v, heads = kv_heads * group: head h reads
  *               key / value head h / group

@@ -165,6 +165,31 @@ __device__ __forceinline__ s16x4 lds_transposed(const bf16_t* p) {
     typedef __attribute__((address_space(3))) s16x4 lds_t;
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)p);
 }
+// Infinities and NaN among a lane's numbers.  Set to zero if `clear`; returns whether there are any (all exponent bits set: one more carries into
+// the sign's place).
+__device__ __forceinline__ bool infinite(float x) { return !(fabsf(x) <= 3.402823466e38f); }
+__device__ __forceinline__ bool infinite(bf16x8& x, bool clear) {
+    union { bf16x8 v; unsigned u[4]; } w;
+    w.v = x;
+    unsigned any = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned carry = ((w.u[i] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+        any |= carry;
+        if (clear) w.u[i] &= ~((carry >> 15) * 0xFFFFu);
+    }
+    if (clear) x = w.v;
+    return any != 0;
+}
+__device__ __forceinline__ bool infinite(f32x4& x, bool clear) {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        any = any || infinite(x[i]);
+        if (clear && infinite(x[i])) x[i] = 0.0f;
+    }
+    return any;
+}
 __device__ __forceinline__ bf16x8 join(s16x4 a, s16x4 b) {
     union { s16x4 h[2]; bf16x8 v; } u;
     u.h[0] = a; u.h[1] = b;
@@ -449,14 +474,17 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
             }
             __syncthreads();                   // the scores are there, q has been read
             if (first + C < end) tq.load(lds_q, end - first - C);
-            // 3. the chunk's own part of the outputs
+            // 3. the chunk's own part of the outputs.  The products take zero times a later frame's v, which is NaN if that is infinite or NaN: such
+            // numbers of v are left out of them and added to the frames that they belong to, one by one.
             if (busy) {
+                bool apart = false;
                 if constexpr (F32) {
 #pragma unroll
                     for (int jt = 0; jt < IT; ++jt) {
                         f32x4 v, pf[IT];
 #pragma unroll
                         for (int r = 0; r < 4; ++r) v[r] = lds_v[(16 * jt + r) * BV + (place<T, BV>(4 * g, 16 * wave + m) ^ 4 * r)];
+                        if (__any(infinite(v, false))) { infinite(v, true); apart = true; }
 #pragma unroll
                         for (int it = jt; it < IT; ++it) pf[it] = *(const f32x4*)(lds_p + score_at(16 * it + m, 16 * jt + 4 * g));
 #pragma unroll
@@ -467,7 +495,8 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
                 } else {
 #pragma unroll
                     for (int s = 0; s < C / 32; ++s) {
-                        const bf16x8 v = v_frames(s);
+                        bf16x8 v = v_frames(s);
+                        if (__any(infinite(v, false))) { infinite(v, true); apart = true; }
 #pragma unroll
                         for (int u = 0; u < OPERAND_PARTS; ++u) {
                             bf16x8 pf[IT];
@@ -477,6 +506,26 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
                             for (int it = 2 * s; it < IT; ++it) acc[it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[it], acc[it], 0, 0, 0);
                         }
                     }
+                }
+                if (apart) {
+                    int frame = m, column = 16 * wave + 4 * g;
+                    asm volatile("" : "+v"(frame), "+v"(column));      // (places are worked out here: kept through the chunks, they would not fit the registers)
+#pragma unroll 1
+                    for (int j = 0; j < rows; ++j)
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const float x = (float)lds_v[place<T, BV>(j, column + u)];
+                            if (!infinite(x)) continue;
+#pragma unroll
+                            for (int it = 0; it < IT; ++it) {
+                                const T* p = lds_p + score_at(16 * it + frame, j);
+                                float score = (float)p[0];
+                                if constexpr (!F32)
+#pragma unroll
+                                    for (int y = 1; y < OPERAND_PARTS; ++y) score += (float)p[y * C * C];
+                                if (j <= 16 * it + frame) acc[it][u] = fmaf(score, x, acc[it][u]);
+                            }
+                        }
                 }
                 const int64_t step = a.reverse ? -a.o.st : a.o.st;
                 const int64_t at = (int64_t)(a.reverse ? L - 1 - first - m : first + m) * a.o.st + n * a.o.sn + h * a.o.sh + out_col;
