@@ -38,7 +38,7 @@ enum rnn_dtype { RNN_F32 = 0, RNN_BF16 = 1, RNN_F16 = 2 };
  *     S(t) = exp(log_decay[h]) S(t - 1) + k(t) v(t)^T          o(t) = scale S(t)^T q(t)
  * that is o(t) = scale sum_{s <= t} exp((t - s) log_decay[h]) (q(t) . k(s)) v(s) + the part of
  * the state before the window.  Frames are worked on together, in chunks (Section 3.1's aim for
- * a recurrence that has no nonlinearity); few frames (up to 4) one after another.  An infinity or NaN in a
+ * a recurrence that has no nonlinearity); few frames (up to 4; up to 8 of heads of less than 16 bytes) one after another.  An infinity or NaN in a
  * frame reaches what the formulas make of that frame, where an infinity may become NaN: outputs and dq of it
  * and later frames, dk and dv of it and earlier ones, of its stream and head.
  *   T, N        frames and streams; T = 0 and N = 0 are allowed

@@ -236,17 +236,18 @@ __device__ __forceinline__ int place(int row, int col) {
 }
 
 // A tile of C frames x D units, brought from memory to LDS by all THREADS.  Frames beyond the last one read the last again (their scores,
-// weights and outputs are left out); what lies behind the units of a row stays zero from the start.  Rows have at least 16 bytes.
+// weights and outputs are left out); what lies behind the units of a row stays zero from the start.
 // DIRECT (rows of whole 16-byte pieces, all aligned to them): straight to LDS, 64 lanes x 16 bytes at once in the order of the lanes, a lane
 // reading the piece that belongs in its place; s_waitcnt vmcnt(0) and a barrier make them visible.  Otherwise through registers, a row's last
-// 16 bytes from where they end.  (128 units, direct / through registers, us: bf16 forward 138 / 190, backward 218 / 342, fp32 backward 607 / 840.)
+// 16 bytes from where they end, rows of less than 16 bytes number by number.  (128 units, direct / through registers, us: bf16 forward 138 / 190, backward 218 / 342, fp32 backward 607 / 840.)
 template <class T, int C, int D, int THREADS, bool DIRECT>
 struct Tile {
     static constexpr int E = 16 / sizeof(T), ROW = D / E, ROWS = THREADS / ROW, PIECES = C / ROWS;      // pieces of a row; rows of a piece of all threads
     static_assert(THREADS % ROW == 0 && C % ROWS == 0, "tile");
-    const T* base; int64_t step; int dim;
+    const T* base; int64_t step; int dim; bool narrow;
     __device__ __forceinline__ Tile(const AttnTensor& a, int n, int h, int unit, int d, bool reverse, int L, int begin) {
         dim = d - unit;      // units of this tile (may be more than D)
+        narrow = d < E;
         step = reverse ? -a.st : a.st;
         base = (const T*)a.p + n * a.sn + (h / a.group) * a.sh + unit + (reverse ? (L - 1) * a.st : 0) + begin * step;
     }
@@ -262,6 +263,15 @@ struct Tile {
                 const int i = row + x * ROWS, at = place<T, D>(i, slot) - i * D;      // (exchanging twice gives back the piece)
                 if (at < dim) __builtin_amdgcn_global_load_lds((global_t)(base + min(i, rows - 1) * step + at), (lds_t)(lds + x * ROWS * D + wave * 64 * E), 16, 0, 0);
             }
+        } else if (narrow) {
+            if (slot == 0)
+                for (int e = 0; e < dim; ++e) {
+                    T v[PIECES];
+#pragma unroll
+                    for (int x = 0; x < PIECES; ++x) v[x] = base[min(row + x * ROWS, rows - 1) * step + e];
+#pragma unroll
+                    for (int x = 0; x < PIECES; ++x) lds[place<T, D>(row + x * ROWS, e)] = v[x];
+                }
         } else {
             u32x4 r[PIECES];
 #pragma unroll
@@ -708,8 +718,11 @@ ChunkShape chunk_shape(int dtype, int dk, int dv) {
 }
 }  // namespace
 
-// Few frames go one after another, and so do heads of less than 16 bytes, which the tiles of chunks cannot load.
-static bool by_frames(const AttnCall& c, const AttnOp& a) { return c.T <= ATTN_STEPS || std::min(a.dk, a.dv) * (c.dtype == DT_F32 ? 4 : 2) < 16; }
+// Few frames go one after another.
+static bool by_frames(const AttnCall& c, const AttnOp& a) {
+    const bool narrow = std::min(a.dk, a.dv) * (c.dtype == DT_F32 ? 4 : 2) < 16;
+    return c.T <= (narrow ? ATTN_STEPS_NARROW : ATTN_STEPS);
+}
 
 int64_t attention_space(const AttnCall& c, const AttnOp* ops, int n_ops) {
     if (n_ops == 0 || by_frames(c, ops[0])) return 0;

@@ -133,3 +133,22 @@ def test_chunks_and_single_frames_agree(dtype):
     assert (np.abs(host(state) - host(c.state_out)) <= 2 * c.tolerance(mag["state_out"], torch.float32, want["state_out"])).all()
     c.x["o"], c.state_out = o, state
     c.check(("o", "state_out"), False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(1, 1), (3, 40), (40, 3), (7, 7), (2, 200), (130, 5)])
+@pytest.mark.parametrize("T,layout", [(5, "frames"), (70, "heads"), (150, "streams"), (1000, "frames")])
+def test_heads_of_less_than_16_bytes(T, layout, dk, dv, dtype):
+    run_and_check(Exact(T, 2, 4, 2, dk, dv, dtype, [T, T - 3], seed=T + dk, layout=layout))
+
+
+@pytest.mark.parametrize("dk,dv", [(3, 3), (16, 16)])
+def test_decays_next_to_one_over_many_frames(dk, dv):
+    """exp(-1e-7) has no neighbour in fp32 nearer than 1.9e-8, which 20,000 frames would make 3.8e-4 of what the first state leaves; bound: 2.6e-5."""
+    c = Exact(20000, 1, 2, 2, dk, dv, "f32", seed=1, decays=[-1e-7, -3e-7])
+    c.state *= 1000
+    c.dstate_out *= 1000
+    c.forward()
+    c.check_norms(("o", "state_out"), False)
+    c.backward()
+    c.check_norms(("dq", "dk", "dv", "dstate"), True)
