@@ -285,7 +285,7 @@ __global__ void count_kernel(int64_t* p, int64_t add, bool fresh) { *p = (fresh 
 template <class T, bool WHOLE>
 __global__ void __launch_bounds__(256) dropout_kernel(DropoutRowsArgs a) {
     constexpr int U = 4;
-    const unsigned groups = (unsigned)(a.dim + 7) / 8;
+    const unsigned groups = ((unsigned)a.dim + 7) / 8;
     const uint64_t total = (uint64_t)a.rows * groups, offset = drop_offset(a.drop);
     const int64_t first_row = a.first_row + (a.d_first_row ? *a.d_first_row : 0);
     for (uint64_t base = (uint64_t)blockIdx.x * (256 * U); base < total; base += (uint64_t)gridDim.x * (256 * U)) {
@@ -384,7 +384,7 @@ hipError_t launch_count(int64_t* p, int64_t add, bool fresh, hipStream_t s) {
 
 hipError_t launch_dropout(int dtype, const DropoutRowsArgs& a, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
-    const int64_t total = a.rows * ((a.dim + 7) / 8);
+    const int64_t total = a.rows * (((int64_t)a.dim + 7) / 8);
     return by_type(dtype, [&](auto* t) {
         typedef std::remove_pointer_t<decltype(t)> T;
         auto* kernel = a.dim % 8 == 0 ? dropout_kernel<T, true> : dropout_kernel<T, false>;

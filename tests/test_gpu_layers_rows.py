@@ -1,0 +1,26 @@
+"""Row layers on the GPU: the widest rows."""
+import pytest
+
+from oracle import layers_oracle as lo
+from tests.test_gpu_layers import DEV
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.mark.parametrize("dim", [(1 << 31) - 8, (1 << 31) - 4, (1 << 31) - 1])
+def test_dropout_of_the_widest_rows(dim):
+    from paper_1503_02852_amd import layers
+    print(f"[dropout] 1 x {dim}", flush=True)
+    x, y = torch.ones(1, dim, device=DEV, dtype=torch.bfloat16), torch.full((1, dim), -7.0, device=DEV, dtype=torch.bfloat16)
+    layers.dropout(x, y, 0.5, 9, 3)
+    groups = -(-dim // 8)
+    for first in (0, groups // 2, groups - 100):
+        want = torch.from_numpy(lo.dropout_factor(100, 8, 0.5, 9, 3, first_row=first)).reshape(-1)      # (rows of eight units: a counter's number is the row's)
+        got = y[0, 8 * first:8 * first + 800].cpu().double()
+        assert torch.equal(got, want[:got.numel()]), first
+    assert int((y < 0).sum()) == 0
+    half = float((y != 0).sum()) / dim
+    assert abs(half - 0.5) < 1e-4      # nine times the deviation of 2^31 draws, 1.1e-5
+    del x, y
+    torch.cuda.empty_cache()
