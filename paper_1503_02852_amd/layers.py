@@ -45,6 +45,13 @@ def _device(device):
     return torch.device("cuda", torch.cuda.current_device() if device.index is None else device.index)
 
 
+def _int32(**sizes):
+    """ctypes cuts numbers off without a word."""
+    for name, n in sizes.items():
+        if not -(1 << 31) <= n < 1 << 31:
+            raise _invalid(f"{name} = {n} does not fit 32 bits")
+
+
 def _dtype(dtype, allowed=DTYPES):
     if dtype not in allowed:
         raise _invalid(f"dtype {dtype} is not one of {', '.join(str(d) for d in allowed)}")
@@ -78,9 +85,10 @@ class LinearAttention:
     """S(t) = exp(log_decay[h]) S(t - 1) + k(t) v(t)^T,  o(t) = scale S(t)^T q(t), for windows of T frames and N streams."""
 
     def __init__(self, T, N, heads, dim_k, dim_v, kv_heads=None, dtype=torch.bfloat16, scale=1.0, training=False, device="cuda:0"):
+        kv_heads = heads if kv_heads is None else kv_heads
+        _int32(T=T, N=N, heads=heads, kv_heads=kv_heads, dim_k=dim_k, dim_v=dim_v)
         self.lib = load_library()
         self.dev, self.dtype = _device(device), dtype
-        kv_heads = heads if kv_heads is None else kv_heads
         self.desc = LinearAttentionDesc(T, N, heads, kv_heads, dim_k, dim_v, _dtype(dtype, (torch.float32, torch.bfloat16)), scale)
         self.ref = C.byref(self.desc)
         self.shapes = {"q": (T, N, heads, dim_k), "k": (T, N, kv_heads, dim_k), "v": (T, N, kv_heads, dim_v), "o": (T, N, heads, dim_v)}
@@ -152,6 +160,7 @@ class AddNorm:
     """h = residual + dropout(x),  y = gain h / sqrt(mean(h^2) + eps), for `rows` rows of `dim` units."""
 
     def __init__(self, rows, dim, dtype=torch.bfloat16, eps=1e-6, dropout=0.0, seed=0, offset=0, d_offset=None, device="cuda:0"):
+        _int32(dim=dim)
         self.lib = load_library()
         self.dev, self.dtype, self.rows, self.dim = _device(device), dtype, rows, dim
         self.d_offset = d_offset      # (kept: the descriptor has its address)
@@ -177,6 +186,7 @@ class AddNorm:
 
     def forward_e4m3(self, x, y, scales, residual=None, gain=None, h=None, rstd=None, group=128):
         """y: torch.float8_e4m3fn; scales: [rows][ceil(dim / 128)], or [rows][1] with group = 0."""
+        _int32(group=group)
         blocks = -(-self.dim // 128) if group else 1
         with _On(self.dev) as stream:
             _check(self.lib.rnn_add_norm_e4m3(self.ref, *self._rows("x", x), *self._rows("residual", residual), self._floats("gain", gain, (self.dim,)),
@@ -196,8 +206,9 @@ class AddNorm:
 
 def dropout(x, y, p, seed, offset=0, d_offset=None):
     """y = x / (1 - p) where the generator keeps an element, else 0; the same call on dy is the gradient.  y may be x."""
-    lib = load_library()
     dim = x.shape[-1] if x.dim() else 1
+    _int32(dim=dim)
+    lib = load_library()
     rows = x.numel() // dim if dim else 0
     px, ld_x = _rows("x", x, rows, dim, x.dtype, _device(x.device))
     py, ld_y = _rows("y", y, rows, dim, x.dtype, x.device)
