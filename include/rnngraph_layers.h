@@ -16,7 +16,7 @@
  *  - Frames x streams tensors are given as rnn_frames: element (t, n, h, i) lies at
  *    data[t * stride_t + n * stride_n + h * stride_h + i], strides in elements, of any sign and size.
  *    Inputs may overlap each other; an output may overlap nothing, and two of its elements may
- *    not share a place.  Alignment: that of the element type.
+ *    not share a place (strides with which neighbours along one or two axes do are refused).  Alignment: that of the element type.
  *  - Sums, statistics and states are fp32 whatever the type of the tensors, and what is stored is rounded once, to
  *    nearest.  Attention on RNN_BF16 tensors multiplies with the matrix instructions for bf16: the scores between frames of
  *    a chunk and, for outputs and gradients, the state that the chunk starts from go there in two bf16 numbers each, which

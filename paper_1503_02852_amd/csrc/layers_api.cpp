@@ -99,6 +99,20 @@ int check_frames(const char* name, const rnn_frames* f, const rnn_linear_attenti
     if (misaligned(f->data, size_of(d->dtype))) return invalid(std::string("attention: ") + name + " is not aligned to its type");
     return RNN_OK;
 }
+// An output, `heads` x `units` for a frame: two of its elements share a place where an axis steps, or two axes' steps differ, by less than a head's units.
+int check_places(const char* name, const rnn_frames* f, const rnn_linear_attention_desc* d, int32_t heads, int32_t units) {
+    if (!f || !f->data) return RNN_OK;
+    typedef __int128 wide;
+    const int32_t size[3] = {d->T, d->N, heads};
+    const wide stride[3] = {f->stride_t, f->stride_n, f->stride_h};
+    const auto small = [&](wide step) { return step > -units && step < units; };
+    bool shared = false;
+    for (int i = 0; i < 3; ++i) {
+        shared = shared || (size[i] > 1 && small(stride[i]));
+        for (int j = 0; j < i; ++j) shared = shared || (size[i] > 1 && size[j] > 1 && (small(stride[i] - stride[j]) || small(stride[i] + stride[j])));
+    }
+    return shared && d->T > 0 ? invalid(std::string("attention: elements of ") + name + " share places") : RNN_OK;
+}
 int check_floats(const char* name, const void* p) { return misaligned(p, 4) ? invalid(std::string("attention: ") + name + " is not aligned to its type") : RNN_OK; }
 
 AttnTensor tensor(const rnn_frames* f, int group) { return f ? AttnTensor{f->data, f->stride_t, f->stride_n, f->stride_h, group} : AttnTensor{nullptr, 0, 0, 0, group}; }
@@ -190,6 +204,7 @@ int rnn_linear_attention_forward(const rnn_linear_attention_desc* d, const rnn_f
         const AttnSpace w = space_of(d, false);
         if (!rc) rc = check_workspace(d_workspace, ws_bytes, w.total);
         if (rc || d->N == 0) return rc;
+        if ((rc = check_places("o", o, d, d->heads, d->dim_v))) return rc;
         AttnOp a = forward_op(d, q, k, v);
         if (with_o) a.o = output(o);
         a.s_in = d_state_in; a.s_out = d_state_out;
@@ -221,6 +236,9 @@ int rnn_linear_attention_backward(const rnn_linear_attention_desc* d, const rnn_
         const AttnSpace w = space_of(d, true);
         if (!rc) rc = check_workspace(d_workspace, ws_bytes, w.total);
         if (rc || d->N == 0) return rc;
+        if ((rc = check_places("dq", dq, d, d->heads, d->dim_k))) return rc;
+        if ((rc = check_places("dk", dk, d, d->kv_heads, d->dim_k))) return rc;
+        if ((rc = check_places("dv", dv, d, d->kv_heads, d->dim_v))) return rc;
         hipStream_t s = static_cast<hipStream_t>(hip_stream);
         const int group = d->heads / d->kv_heads;
         const AttnCall call = call_of(d, d_log_decay, d_lengths);

@@ -143,3 +143,22 @@ def test_misaligned_vectors_are_refused():
     for p in (P + 1, P + 4):
         refused(lib.rnn_dropout(drop(d_offset=p), P, 40, P, 40, None), "offset")
         refused(lib.rnn_add_norm_forward(norm(dropout=0.5, d_offset=p), P, 40, None, 0, None, None, 0, P, 40, None, None), "offset")
+
+
+@pytest.mark.parametrize("strides,sizes,shared", [
+    ((0, 48, 24), {}, True), ((512, 0, 24), {}, True), ((512, 96, 0), {}, True), ((512, 96, 23), {}, True), ((512, -23, 96), {}, True),
+    ((96, 96, 24), {}, True), ((-96, 96, 24), {}, True), ((96, 512, 90), {}, True), ((-(1 << 63), 96, 24), {"T": 2}, False), (((1 << 63) - 1, 1 << 62, 24), {}, False),
+    ((0, 96, 24), {"T": 1}, False), ((192, 0, 24), {"N": 1}, False), ((192, 96, 24), {}, False), ((-192, -96, -24), {}, False), ((24, 24 * 8, 24 * 16), {}, False)])
+def test_outputs_whose_elements_share_places_are_refused(strides, sizes, shared):
+    """The others are looked at without a launch: by a call that has nothing to do, and, through the next check, one whose other output is refused."""
+    lib = load_library()
+    f, d = frames(), attention(**dict(dict(kv_heads=4, dim_k=24), **sizes))
+    out, flat = C.byref(Frames(P, *strides)), C.byref(Frames(P, 0, 0, 0))
+    if shared:
+        refused(lib.rnn_linear_attention_forward(d, f, f, f, P, None, None, None, out, P, 1 << 30, None), "o share places")
+    for i, name in enumerate(("dq", "dk", "dv")):      # looked at in this order
+        outs = [out] * i + [out] + [flat] * (2 - i)
+        if shared:
+            refused(lib.rnn_linear_attention_backward(d, f, f, f, P, None, None, f, None, *([None] * i), *outs[i:], None, P, 1 << 30, None), f"{name} share places")
+        elif i < 2:
+            refused(lib.rnn_linear_attention_backward(d, f, f, f, P, None, None, f, None, *outs, None, P, 1 << 30, None), f"{('dk', 'dv')[i]} share places")
