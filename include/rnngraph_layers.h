@@ -78,7 +78,8 @@ int rnn_linear_attention_backward(const rnn_linear_attention_desc* desc, const r
  * For every row of dim units
  *     h = residual + drop(x)        y = gain h / sqrt(mean(h^2) + eps)
  * Element (r, i) of a tensor lies at data[r * ld + i], ld >= dim; an output may be the input of the
- * same call that it replaces (h: residual or x; y: x; likewise the gradients), with the same ld.
+ * same call that it replaces (h: residual or x; y: x or residual; dx and dresidual: dy, dh or h), with the same ld (another one is
+ * refused, and so are two outputs in one place).
  *   rows >= 0, dim 1 .. 16384; dtype of x, residual, h, y: any of rnn_dtype
  *   dropout, seed, offset, d_offset: as in rnn_dropout; dropout = 0: none
  *   d_residual, d_gain (float [dim]) may be NULL: zero, one
@@ -96,7 +97,7 @@ int rnn_add_norm_forward(const rnn_add_norm_desc* desc, const void* d_x, int64_t
 
 /* The same with y in 8 bits (e4m3: four exponent and three mantissa bits, largest value 448) and float scales: y = scale * y8.
  * A scale for every row (group = 0, d_scales [rows]) or for every 128 units of a row (group = 128, d_scales [rows][ceil(dim / 128)]):
- * the largest |y| / 448, or 1 where all are zero. */
+ * the largest |y| / 448, or 1 where all are zero.  y8 may not be an input. */
 int rnn_add_norm_e4m3(const rnn_add_norm_desc* desc, const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual,
                       const float* d_gain, void* d_h, int64_t ld_h, uint8_t* d_y8, int64_t ld_y8, float* d_scales, int32_t group,
                       float* d_rstd, void* hip_stream);

@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdlib>
+#include <initializer_list>
 #include <new>
 
 #include "layers.h"
@@ -54,6 +55,20 @@ int check_row_tensor(const char* name, const void* p, int64_t ld, int64_t rows, 
     if (misaligned(p, bytes)) return invalid(std::string(name) + " is not aligned to its type");
     return RNN_OK;
 }
+// An output in an input's place is written row by row behind what is read: rows have to begin at the same places, and two outputs at different ones.
+struct Place { const char* name; const void* p; int64_t ld; };
+int check_places(int64_t rows, std::initializer_list<Place> outputs, std::initializer_list<Place> inputs, bool may_replace = true) {
+    if (rows == 0) return RNN_OK;
+    for (const Place& a : outputs) {
+        if (!a.p) continue;
+        for (const Place& b : outputs)
+            if (&a != &b && a.p == b.p) return invalid(std::string(a.name) + " and " + b.name + " are one place");
+        for (const Place& b : inputs)
+            if (a.p == b.p && (!may_replace || (rows > 1 && a.ld != b.ld)))
+                return invalid(std::string(a.name) + " may not be " + b.name + (may_replace ? " with another ld" : ""));
+    }
+    return RNN_OK;
+}
 int check_norm(const rnn_add_norm_desc* d) {
     if (!d) return invalid("descriptor is NULL");
     if (const int rc = check_rows(d->rows, d->dim, d->dtype, d->dropout, d->d_offset)) return rc;
@@ -73,6 +88,8 @@ int add_norm(const rnn_add_norm_desc* d, const void* x, int64_t ld_x, const void
     if (!rc) rc = check_row_tensor("gain", gain, d->dim, 1, d->dim, 4, false);
     if (!rc) rc = check_row_tensor("rstd", rstd, d->dim, 1, d->dim, 4, false);
     if (!rc) rc = check_row_tensor("scales", scales, d->dim, 1, d->dim, 4, false);
+    if (!rc) rc = check_places(d->rows, {{"h", h, ld_h}, {"y", y, ld_y}}, {{"x", x, ld_x}, {"residual", residual, ld_residual}});
+    if (!rc && scales) rc = check_places(d->rows, {{"y in 8 bits", y, ld_y}}, {{"x", x, ld_x}, {"residual", residual, ld_residual}}, false);
     if (rc) return rc;
     AddNormArgs a = {};
     a.rows = d->rows; a.dim = d->dim; a.eps = d->eps; a.drop = dropout_args(d->dropout, d->seed, d->offset, d->d_offset);
@@ -301,6 +318,7 @@ int rnn_add_norm_backward(const rnn_add_norm_desc* d, const void* d_dy, int64_t 
         if (!rc) rc = check_row_tensor("rstd", d_rstd, d->dim, d->rows, d->dim, 4, true);
         if (!rc) rc = check_row_tensor("gain", d_gain, d->dim, 1, d->dim, 4, false);
         if (!rc) rc = check_row_tensor("dgain", d_dgain, d->dim, 1, d->dim, 4, false);
+        if (!rc) rc = check_places(d->rows, {{"dx", d_dx, ld_dx}, {"dresidual", d_dresidual, ld_dresidual}}, {{"dy", d_dy, ld_dy}, {"dh", d_dh, ld_dh}, {"h", d_h, ld_h}});
         const int blocks = norm_grad_blocks(d->rows, d->dim);
         if (!rc && d_dgain && blocks > 1) rc = check_workspace(d_workspace, ws_bytes, align_up((int64_t)blocks * d->dim * 4));
         if (rc || (!d_dx && !d_dresidual && !d_dgain)) return rc;
@@ -320,6 +338,7 @@ int rnn_dropout(const rnn_dropout_desc* d, const void* d_x, int64_t ld_x, void* 
         const int b = size_of(d->dtype);
         int rc = check_row_tensor("x", d_x, ld_x, d->rows, d->dim, b, true);
         if (!rc) rc = check_row_tensor("y", d_y, ld_y, d->rows, d->dim, b, true);
+        if (!rc) rc = check_places(d->rows, {{"y", d_y, ld_y}}, {{"x", d_x, ld_x}});
         if (rc) return rc;
         const DropoutRowsArgs a{d->rows, d->dim, dropout_args(d->p, d->seed, d->offset, d->d_offset), RowTensor{const_cast<void*>(d_x), ld_x}, RowTensor{d_y, ld_y}, 0, nullptr};
         return done(launch_dropout(d->dtype, a, static_cast<hipStream_t>(hip_stream)), "dropout launch");

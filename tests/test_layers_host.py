@@ -162,3 +162,22 @@ def test_outputs_whose_elements_share_places_are_refused(strides, sizes, shared)
             refused(lib.rnn_linear_attention_backward(d, f, f, f, P, None, None, f, None, *([None] * i), *outs[i:], None, P, 1 << 30, None), f"{name} share places")
         elif i < 2:
             refused(lib.rnn_linear_attention_backward(d, f, f, f, P, None, None, f, None, *outs, None, P, 1 << 30, None), f"{('dk', 'dv')[i]} share places")
+
+
+def test_outputs_in_the_place_of_inputs():
+    """Row by row, or refused: rows that begin elsewhere, or are shorter (8 bits), would be written while others still read them."""
+    lib = load_library()
+    Q, R = 2 * P, 3 * P
+    f, g, b = lib.rnn_add_norm_forward, lib.rnn_add_norm_e4m3, lib.rnn_add_norm_backward
+    refused(f(norm(), P, 48, None, 0, None, None, 0, P, 40, None, None), "y may not be x with another ld")
+    refused(f(norm(), P, 40, Q, 48, None, None, 0, Q, 40, None, None), "y may not be residual with another ld")
+    refused(f(norm(), P, 40, Q, 48, None, Q, 40, R, 40, None, None), "h may not be residual with another ld")
+    refused(f(norm(), P, 40, None, 0, None, P, 48, R, 40, None, None), "h may not be x with another ld")
+    refused(f(norm(), P, 40, None, 0, None, R, 40, R, 40, None, None), "h and y are one place")
+    for x, res, h in ((R, None, None), (P, R, None), (P, None, R), (P, R, R)):
+        refused(g(norm(), x, 40, res, 40, None, h, 40, R, 40, P, 128, None, None), "y")
+    refused(b(norm(), P, 48, None, 0, Q, 40, P, None, P, 40, None, 0, None, None, 0, None), "dx may not be dy with another ld")
+    refused(b(norm(), P, 40, R, 48, Q, 40, P, None, None, 0, R, 40, None, None, 0, None), "dresidual may not be dh with another ld")
+    refused(b(norm(), P, 40, None, 0, Q, 48, P, None, Q, 40, None, 0, None, None, 0, None), "dx may not be h with another ld")
+    refused(b(norm(), P, 40, None, 0, Q, 40, P, None, R, 40, R, 40, None, None, 0, None), "dx and dresidual are one place")
+    refused(lib.rnn_dropout(drop(), P, 48, P, 40, None), "y may not be x with another ld")
