@@ -2,7 +2,9 @@
 
 Frames x streams tensors are [T][N][heads][units] with any strides but 1 between a head's units; row tensors are
 [..., units], rows evenly spaced.  Calls are queued on the current stream of the tensors' device; what a call needs
-as workspace comes from torch's allocator, for that call and stream alone.  There is no CPU path."""
+as workspace comes from torch's allocator, for that call and stream alone.  There is no CPU path.  Nothing is recorded
+for torch.autograd, the gradients are calls of their own: a tensor that requires gradients is refused where they are
+recorded, as in torch's functions with out= (use torch.no_grad(), detach() or a torch.autograd.Function)."""
 from __future__ import annotations
 
 import ctypes as C
@@ -58,9 +60,15 @@ def _dtype(dtype, allowed=DTYPES):
     return DTYPES[dtype]
 
 
+def _no_record(name, x):
+    if x.requires_grad and torch.is_grad_enabled():
+        raise _invalid(f"{name} requires gradients, which are not recorded here")
+
+
 def _tensor(name, x, shape, dtype, device):
     if x.dtype is not dtype or x.shape != shape or x.device != device:
         raise _invalid(f"{name}: expected {dtype} {list(shape)} on {device}, got {x.dtype} {list(x.shape)} on {x.device}")
+    _no_record(name, x)
     return x
 
 
@@ -139,6 +147,7 @@ def _rows(name, x, rows, dim, dtype, device):
         return None, 0
     if x.dtype is not dtype or x.device != device or x.dim() < 1 or x.shape[-1] != dim or x.numel() != rows * dim:
         raise _invalid(f"{name}: expected {dtype}, {rows} rows of {dim} on {device}, got {x.dtype} {list(x.shape)} on {x.device}")
+    _no_record(name, x)
     if x.is_contiguous():
         return x.data_ptr(), dim
     if dim > 1 and x.stride(-1) != 1:
