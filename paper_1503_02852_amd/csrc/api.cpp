@@ -398,9 +398,21 @@ struct rnn_graph {
     Layout cached_layout;
     int cached_T = 0, cached_N = 0;
     // What rnn_set_attention and rnn_set_dropout gave, per Plan::layers; frames of the window that the attention layers' running states cover (-1: unknown).
+    // A captured call runs later, any number of times, and leaves these states behind its own frames: what an earlier call has left is relied on within
+    // one capture (the same id; 0: none), or between calls that run at once as long as none has been captured.
     struct LayerSetting { int heads = 0; float scale = 1.0f; const float* d_log_decay = nullptr; float p = 0.0f; uint64_t seed = 0, offset = 0; const uint64_t* d_offset = nullptr; };
     std::vector<LayerSetting> layer_settings;
     int attention_upto = -1;
+    unsigned long long attention_capture = 0, capture = 0;      // capture that attention_upto was set in; that of the call that runs
+    bool captured = false;
+    void note_capture(hipStream_t s) {
+        hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+        unsigned long long id = 0;
+        if (hipStreamGetCaptureInfo(s, &status, &id) != hipSuccess) (void)hipGetLastError();      // (the default stream beside a capture)
+        capture = status == hipStreamCaptureStatusActive ? id + 1 : 0;
+        captured = captured || capture != 0;
+    }
+    bool states_reach(int t) const { return attention_upto == t && (capture != 0 ? attention_capture == capture : !captured); }
     rnn_linear_attention_desc attention_desc(int i, int T, int N) const {
         const LayerSetting& ls = layer_settings[i];
         const int dim = plan.xnodes[plan.layers[i].node].dim;
@@ -1367,7 +1379,7 @@ int layer_forward(rnn_graph* g, int i, int t0, int t1, hipStream_t s) {
         float* reached = reinterpret_cast<float*>(g->ws + g->layout.reached_off[i]);
         const int H = g->hist();
         int rc = RNN_OK;
-        if (t0 > H && g->attention_upto != t0 - H) rc = run_attention(g, i, start, reached, H, t0, false, s);
+        if (t0 > H && !g->states_reach(t0 - H)) rc = run_attention(g, i, start, reached, H, t0, false, s);
         if (rc == RNN_OK) rc = run_attention(g, i, t0 > H ? reached : start, reached, t0, t1, true, s);
         if (rc != RNN_OK) return rc;
     } else if (lp.kind == NODE_NORM) {
@@ -1537,6 +1549,7 @@ int rnn_forward_range(rnn_graph* g, const float* d_weights, const float* const* 
         if (e != hipSuccess) return fail_hip(e, "XCD probe");
     }
     const int H = P.hist;
+    if (!P.layers.empty()) g->note_capture(s);
     if (t_begin == 0) {
         // A new window: the control words (loss, error flags) start at zero, and so do the history
         // frames in front of every frame tensor (the state before a fresh window is zero).  Pieces
@@ -1591,6 +1604,7 @@ int rnn_forward_range(rnn_graph* g, const float* d_weights, const float* const* 
         if (rc != RNN_OK) { g->attention_upto = -1; return rc; }
     }
     g->fwd_upto = g->attention_upto = t_end;
+    g->attention_capture = g->capture;
     g->fwd_done = t_end == T;
     return RNN_OK;
 }
@@ -1749,6 +1763,8 @@ int rnn_shift_window(rnn_graph* g, int32_t frames, void* hip_stream) {
     if (e == hipSuccess) e = launch_shift_frames(st, frames, Ti, s);
     if (e != hipSuccess) return fail_hip(e, "window shift");
     g->fwd_upto = g->attention_upto = g->T - frames;
+    if (!P.layers.empty()) g->note_capture(s);
+    g->attention_capture = g->capture;
     g->fwd_done = g->bptt_done = false;
     return RNN_OK;
 }
