@@ -50,3 +50,37 @@ def test_tensors_that_require_gradients():
     y.backward(x["do"])
     for leaf, name in zip(leaves, ("dq", "dk", "dv")):
         assert torch.equal(leaf.grad, x[name]), name
+
+
+def test_rows_over_several_axes():
+    """Values of rows that lie in three and four axes, packed and padded, one axis of one; rows that are not evenly spaced are refused."""
+    import numpy as np
+    from paper_1503_02852_amd import RnnError, layers
+    t, r = torch.bfloat16, np.random.default_rng(0)
+    flat, res = rows_of(r, 24, 40, t), rows_of(r, 24, 40, t)
+    layer = layers.AddNorm(24, 40, dtype=t, dropout=0.25, seed=3, device=DEV)
+    y, h, d = (torch.full((24, 40), -7.0, device=DEV, dtype=t) for _ in range(3))
+    layer.forward(flat, y, residual=res, h=h)
+    layers.dropout(flat, d, 0.5, 4)
+    assert not (y == -7.0).any() and not torch.equal(y, h)
+    for shape in ((4, 6, 40), (2, 3, 4, 40), (24, 1, 40), (1, 24, 1, 40)):
+        padded = lambda: torch.full(shape[:-1] + (48,), -7.0, device=DEV, dtype=t)  # noqa: E731
+        x3, r3, y3, h3, d3 = (padded() for _ in range(5))
+        x3[..., :40], r3[..., :40] = flat.view(shape), res.view(shape)
+        layer.forward(x3[..., :40], y3[..., :40], residual=r3[..., :40], h=h3[..., :40])
+        layers.dropout(x3[..., :40], d3[..., :40], 0.5, 4)
+        for got, want in ((y3, y), (h3, h), (d3, d)):
+            assert torch.equal(got[..., :40].reshape(24, 40), want) and (got[..., 40:] == -7.0).all(), shape
+        packed = torch.full(shape, -7.0, device=DEV, dtype=t)
+        layer.forward(flat.view(shape), packed, residual=r3[..., :40])
+        assert torch.equal(packed.view(24, 40), y), shape
+    x3, y3 = flat.view(4, 6, 40), torch.empty(4, 6, 40, device=DEV, dtype=t)
+    for x in (x3.transpose(0, 1), torch.empty(4, 12, 40, device=DEV, dtype=t)[:, :6]):
+        with pytest.raises(RnnError, match="evenly spaced"):
+            layer.forward(x, y3)
+        with pytest.raises(RnnError, match="evenly spaced"):
+            layer.forward(x3, x)
+    with pytest.raises(RnnError, match="next to each other"):
+        layer.forward(torch.empty(24, 80, device=DEV, dtype=t)[:, ::2], y)
+    with pytest.raises(RnnError, match="ld is less"):
+        layer.forward(flat[:1].expand(24, 40), y)

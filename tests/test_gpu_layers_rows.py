@@ -50,3 +50,41 @@ def test_every_output_in_the_place_of_every_input(dim, dtype):
             t = [dy.clone(), dh.clone(), h.clone()]
             layer.backward(t[0], t[2], rstd, dh=t[1], dx=t[i], dresidual=t[j])
             assert torch.equal(t[i], dx) and torch.equal(t[j], dr), (i, j)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("dim", [1, 100, 129, 600, 1024, 2048, 4096, 5000, 16384])
+def test_e4m3_with_everything(dim, group, dtype):
+    """Every type, with gain, dropout, the sum and rstd stored, rows further apart than they are long; the same y as the call that stores it in the inputs' type."""
+    import numpy as np
+    from paper_1503_02852_amd import layers
+    from tests.test_gpu_layers import U, half_step, host, rows_of, sum_bound
+    r, rows, seed, p = np.random.default_rng(dim), 5, 77 + dim, 0.25
+    x, res, gain = rows_of(r, rows, dim, dtype, dim + 5), rows_of(r, rows, dim, dtype, dim + 8, scale=2.0), torch.from_numpy(r.uniform(0.5, 2.0, dim).astype(np.float32)).to(DEV)
+    blocks = -(-dim // 128) if group else 1
+    y = torch.full((rows, dim + 9), 0.5, device=DEV).to(torch.float8_e4m3fn)
+    h, rstd, scales = torch.full((rows, dim + 3), -7.0, device=DEV, dtype=dtype), torch.empty(rows, device=DEV), torch.empty(rows, blocks, device=DEV)
+    layer = layers.AddNorm(rows, dim, dtype=dtype, eps=1e-5, dropout=p, seed=seed, offset=5, device=DEV)
+    layer.forward_e4m3(x, y[:, :dim], scales, residual=res, gain=gain, h=h[:, :dim], rstd=rstd, group=group)
+    assert (y.float()[:, dim:] == 0.5).all() and (h[:, dim:] == -7.0).all()
+    factor = lo.dropout_factor(rows, dim, p, seed, 5)
+    H, Y, R = lo.add_norm(host(x), host(res), host(gain), np.float32(1e-5), factor)
+    dh = sum_bound(dim, factor, host(x), host(res))
+    assert (np.abs(host(h[:, :dim]) - H) <= dh + half_step(dtype) * np.abs(H) + torch.finfo(dtype).tiny).all()
+    dr = (U * (dim / 2 + 16) * np.ones(rows) + (dh * np.abs(H)).sum(1) / (H * H).sum(1)) * R      # as in the test of the norm itself
+    assert (np.abs(host(rstd) - R) <= dr).all()
+    dy = (np.abs(H) * dr[:, None] + dh * R[:, None] + 4 * U * np.abs(H) * R[:, None]) * np.abs(host(gain))
+    width = 128 if group else dim
+    cut = [slice(b * width, min((b + 1) * width, dim)) for b in range(blocks)]
+    most = np.stack([np.abs(Y[:, c]).max(1) for c in cut], 1)
+    assert (np.abs(host(scales) - most / 448) <= np.stack([dy[:, c].max(1) for c in cut], 1) / 448 + 2 * U * most / 448).all()
+    s = np.repeat(host(scales), width, 1)[:, :dim]
+    q = host(y[:, :dim].float())
+    # e4m3: half a step of 2^-4 relative, below 2^-6 steps of 2^-9; the quotient's two roundings and the scale's
+    assert (np.abs(q * s - Y) <= np.maximum(2.0 ** -4 * np.abs(Y), 2.0 ** -10 * s) * (1 + 2.0 ** -10) + dy + 4 * U * np.abs(Y)).all()
+    assert (np.abs(q).max(1) == 448).all()
+    want = torch.empty(rows, dim, device=DEV, dtype=dtype)
+    h2, rstd2 = torch.empty(rows, dim, device=DEV, dtype=dtype), torch.empty_like(rstd)
+    layer.forward(x, want, residual=res, gain=gain, h=h2, rstd=rstd2)
+    assert torch.equal(h[:, :dim], h2) and torch.equal(rstd, rstd2)
