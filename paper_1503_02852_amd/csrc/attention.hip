@@ -182,13 +182,13 @@ __device__ __forceinline__ bool infinite(bf16x8& x, bool clear) {
     return any != 0;
 }
 __device__ __forceinline__ bool infinite(f32x4& x, bool clear) {
-    bool any = false;
+    float none = 0.0f;      // times zero: NaN if there is one
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        any = any || infinite(x[i]);
+        none = fmaf(x[i], 0.0f, none);
         if (clear && infinite(x[i])) x[i] = 0.0f;
     }
-    return any;
+    return none != 0.0f;
 }
 __device__ __forceinline__ bf16x8 join(s16x4 a, s16x4 b) {
     union { s16x4 h[2]; bf16x8 v; } u;
@@ -494,9 +494,9 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
                         f32x4 v, pf[IT];
 #pragma unroll
                         for (int r = 0; r < 4; ++r) v[r] = lds_v[(16 * jt + r) * BV + (place<T, BV>(4 * g, 16 * wave + m) ^ 4 * r)];
-                        if (__any(infinite(v, false))) { infinite(v, true); apart = true; }
 #pragma unroll
                         for (int it = jt; it < IT; ++it) pf[it] = *(const f32x4*)(lds_p + score_at(16 * it + m, 16 * jt + 4 * g));
+                        if (__any(infinite(v, false))) { infinite(v, true); apart = true; }
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -506,12 +506,12 @@ __global__ void __launch_bounds__(64 * W, (chunk_waves(sizeof(T) == 4, DK, DIREC
 #pragma unroll
                     for (int s = 0; s < C / 32; ++s) {
                         bf16x8 v = v_frames(s);
-                        if (__any(infinite(v, false))) { infinite(v, true); apart = true; }
 #pragma unroll
                         for (int u = 0; u < OPERAND_PARTS; ++u) {
                             bf16x8 pf[IT];
 #pragma unroll
                             for (int it = 2 * s; it < IT; ++it) pf[it] = *(const bf16x8*)(lds_p + u * C * C + score_at(16 * it + m, 32 * s + 8 * g));
+                            if (u == 0 && __any(infinite(v, false))) { infinite(v, true); apart = true; }
 #pragma unroll
                             for (int it = 2 * s; it < IT; ++it) acc[it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[it], acc[it], 0, 0, 0);
                         }
