@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(256) attention_steps_kernel(AttnCall c, StepOp
 // state as an operand of the outputs, in OPERAND_PARTS = 2: 2^-16 of a term is lost at most (the upper eight bits are cut off, the rest is rounded to
 // eight), which is what 256 of the fp32 additions that make a result (some 4 (dk + dv) + 8 a frame between) may take.  In one number 2^-9 of a term
 // would be lost, which results whose terms cancel (keys and values around one, queries that sum up to nothing) do not stand.  In one / two / three,
-// us, 2,048 frames x 8 streams x 16 heads x 128 x 128, forward and backward: 136, 227 / 141, 253 / 151, 282; 65,536 frames, 8 heads: 194 / 209 / 226.
+// us, 2,048 frames x 8 streams x 16 heads x 128 x 128, forward: 132 / 134 / 141, backward: 221 / 251 / 271; 65,536 frames, 8 heads: 197 / 209 / 223.
 // ---------------------------------------------------------------------------------------------
 typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
 typedef bf16_t bf16x4 __attribute__((ext_vector_type(4)));
@@ -146,12 +146,13 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-// Measured, 2,048 frames x 8 streams x 16 heads x 128 x 128 units, bf16: forward 136 us, backward 217 us (0.45 GB moved, 0.10 TFLOP: a third of the
-// memory's rate, a third of the matrix cores').  Without loads and stores backward takes 168 us, of which the state's update is 64 (as many vector
-// instructions for V' as matrix instructions), the state's part of the outputs 28, the scores 24, their product with V 25: a workgroup's phases follow
-// each other, and what a second one on the compute unit fills in is limited by the 384 workgroups there are for 256 compute units.  Half the LDS
-// reads (32 columns to a wavefront), keys a chunk ahead and one barrier fewer changed nothing; chunks of 32 frames take 220 us.
-// fp32: 607 us, 64 GFLOP at 0.75 of the fp32 matrix rate.
+// Measured, 2,048 frames x 8 streams x 16 heads x 128 x 128 units, bf16: forward 134 us, backward 251 us (0.45 GB moved, 0.15 TFLOP on the matrix cores
+// with the parts: a third of the memory's rate, half of the matrix cores').  With neither loads nor stores it takes 190 where it took 239; without the
+// state's update 63 less than that (as many vector instructions for V' as matrix instructions), without the state's part of the outputs 46, without the
+// scores 25, without their product with V 28: a workgroup's phases follow each other, and what a second one on the compute unit fills in is limited by
+// the 384 workgroups there are for 256 compute units.  Half the LDS reads (32 columns to a wavefront), keys a chunk ahead and one barrier fewer changed
+// nothing (with scores and state in one part).  fp32: forward 287 us, backward 616 us, 64 GFLOP at 0.74 of the fp32 matrix rate.
+// (Figures of one list come from one run; where a call's tensors lie moves them by up to 5 %.)
 struct ChunkOps {
     AttnOp op[3];
     float* seg_state[3];      // [segment][stream, head][dk][dv]: what a segment adds to the state, then the state before it
@@ -222,8 +223,8 @@ __device__ __forceinline__ void split(F x, B (&part)[N]) {
     part[N - 1] = __builtin_convertvector(x, B);
 }
 
-// Frames of a chunk: as many as leave LDS room for two workgroups.  (bf16, 128 units, with 64 / 32: forward 136 / 142, backward 217 / 220, 4,096
-// frames of one stream 55.5 / 57.5, 16 streams forward 166 / 178 us.)
+// Frames of a chunk: as many as leave LDS room for two workgroups.  (bf16, 128 units, with 64 / 32: forward 134 / 144, backward 251 / 268, 4,096
+// frames of one stream 57 / 62, 16 streams forward 187 / 198 us.)
 constexpr int chunk_frames(bool f32, int DK) { return f32 || DK > 128 ? 32 : 64; }
 
 // Place of (frame, unit) of a tile of D units in LDS: the 16-byte pieces of a row are exchanged, so that neither 16 bytes of eight frames
@@ -239,7 +240,7 @@ __device__ __forceinline__ int place(int row, int col) {
 // weights and outputs are left out); what lies behind the units of a row stays zero from the start.
 // DIRECT (rows of whole 16-byte pieces, all aligned to them): straight to LDS, 64 lanes x 16 bytes at once in the order of the lanes, a lane
 // reading the piece that belongs in its place; s_waitcnt vmcnt(0) and a barrier make them visible.  Otherwise through registers, a row's last
-// 16 bytes from where they end, rows of less than 16 bytes number by number.  (128 units, direct / through registers, us: bf16 forward 138 / 190, backward 218 / 342, fp32 backward 607 / 840.)
+// 16 bytes from where they end, rows of less than 16 bytes number by number.  (128 units, direct / through registers, us: bf16 forward 134 / 178, backward 251 / 392, fp32 backward 616 / 879.)
 template <class T, int C, int D, int THREADS, bool DIRECT>
 struct Tile {
     static constexpr int E = 16 / sizeof(T), ROW = D / E, ROWS = THREADS / ROW, PIECES = C / ROWS;      // pieces of a row; rows of a piece of all threads
@@ -688,9 +689,9 @@ static hipError_t launch_attention_steps(const AttnCall& c, const AttnOp* ops, i
 
 // Segments of the frames, so that the chip is filled (two workgroups to a compute unit) where streams and heads are few: each adds its frames up to a
 // state of its own, a scan makes these the states in front of the segments, and the outputs of all are worked out at once.  That reads k and v twice.
-// Whole / in segments, us, heads of 128 x 128 in bf16: 4,096 frames, 16 heads 260 / 55; 65,536 frames, 8 heads 4016 / 195; 2,048 frames x 8 streams x 16
-// heads forward (128 workgroups) 156 / 140; backward (384) 217 / 299: from 256 on they stay whole.  For 256, 512, 1,024 workgroups: 55, 55, 55; 240, 195, 208;
-// 150, 140, 171.  Segments of at least 2, 4, 8 chunks: 58, 55, 72 (4,096 frames).
+// Whole / in segments, us, heads of 128 x 128 in bf16: 4,096 frames, 16 heads 294 / 57; 65,536 frames, 8 heads 4536 / 209; 2,048 frames x 8 streams x 16
+// heads forward (128 workgroups) 157 / 134; backward (384) 251 / 314: from 256 on they stay whole.  For 256, 512, 1,024 workgroups: 57, 57, 57; 245, 209, 226;
+// 143, 134, 165.  Segments of at least 2, 4, 8 chunks: 62, 57, 76 (4,096 frames).
 static int64_t most_segments(int T, int64_t works, int C) {      // (grows with T: room for a window's is room for a part's)
     const int64_t chunks = (T + C - 1) / C;
     return std::max<int64_t>(1, works >= 256 || works == 0 ? 1 : std::min<int64_t>((512 + works - 1) / works, chunks / 4));
@@ -707,9 +708,9 @@ ChunkShape chunk_shape(int dtype, int dk, int dv) {
     ChunkShape s;
     s.DK = dk <= 64 ? 64 : dk <= 128 ? 128 : 256;
     // Columns of a workgroup: 64, or 128 (half as many reads of q and k, scores worked out once; fewer workgroups on a compute unit, which hide each
-    // other's waits less).  128 / 64 columns, us, 2,048 frames x 8 streams x 16 heads, forward and backward: bf16 128 x 128 units 124 / 125, 206 / 220,
-    // 256 x 256 232 / 242, 626 / 585; fp32 64 x 128 216 / 206, 673 / 609 (4,096 frames, one stream 250 / 289), 128 x 128 328 / 282, 806 / 626,
-    // 128 x 256 404 / 430, 256 x 256 750 / 843, 2217 / 2483.
+    // other's waits less).  128 / 64 columns, us, 2,048 frames x 8 streams x 16 heads, forward and backward: bf16 128 x 128 units 133 / 130, 244 / 293,
+    // 256 x 256 287 / 288, 771 / 718; fp32 64 x 128 185 / 194, 688 / 607 (4,096 frames, one stream 256 / 291), 128 x 128 332 / 287, 828 / 615,
+    // 128 x 256 414 / 444, 2221 / 2340, 256 x 256 758 / 800, 2246 / 2358.
     const bool half = dv <= 64 || (dtype == DT_F32 ? s.DK == 128 && dv <= 128 : s.DK == 256);
     s.W = half ? 4 : 8;
     s.C = chunk_frames(dtype == DT_F32, s.DK);

@@ -69,8 +69,9 @@ struct AttnOp {
 struct AttnCall { int T, N, heads, dtype; const float* log_decay; const int32_t* lengths; };
 constexpr int ATTN_MAX_DIM = 256;
 // Windows of at most so many frames go frame by frame, longer ones in chunks.  Frame by frame / in chunks, us for T = 2, 4, 8 (in a graph):
-// 64 streams x 16 heads x 128 x 128, bf16: 29 / 33, 37 / 34, 52 / 34;  64 x 64, bf16: 9.5 / 13.8, 12.4 / 13.9, 18.4 / 13.9;
-// 64 x 8 heads x 128 x 128, fp32: 20 / 32, 26 / 31, 38 / 31;  one stream, 16 heads x 128 x 128, bf16: 6.6 / 9.6, 9.7 / 9.6, 15.9 / 9.6.
+// 64 streams x 16 heads x 128 x 128, bf16: 29 / 36, 37 / 35, 51 / 36;  64 x 64, bf16: 9.5 / 17.5, 12.5 / 17.7, 18.1 / 17.8;
+// 64 x 8 heads x 128 x 128, fp32: 20 / 31, 25 / 31, 38 / 31;  one stream, 16 heads x 128 x 128, bf16: 6.7 / 10.4, 9.7 / 10.4, 16.0 / 10.4;
+// backward, 16 x 16 heads x 128 x 128, bf16: 33 / 38, 41 / 38, 55 / 39.
 constexpr int ATTN_STEPS = 4;
 // Heads of less than 16 bytes (their tiles are loaded number by number), T = 6, 8, 16, 1,024: 64 streams x 16 heads x 4 x 4, bf16: 13.3 / 17.1, 16.2 / 17.0,
 // 27 / 17.0, 1,352 / 143;  one stream: 9.1 / 9.2, 11.1 / 9.2, 19.3 / 9.2, 1,024 / 34;  64 x 16 heads x 3 x 3, fp32: 13.3 / 16.5, 15.9 / 16.5, 26 / 16.6, 1,257 / 287.
