@@ -15,8 +15,9 @@
  *    of their own: two streams, or two captured graphs that are replayed at the same time.
  *  - Frames x streams tensors are given as rnn_frames: element (t, n, h, i) lies at
  *    data[t * stride_t + n * stride_n + h * stride_h + i], strides in elements, of any sign and size.
- *    Inputs may overlap each other; an output may overlap nothing, and two of its elements may
- *    not share a place (strides with which neighbours along one or two axes do are refused).  Alignment: that of the element type.
+ *    Inputs may overlap each other; an output may overlap nothing (where it begins at an input or another
+ *    output the call is refused), and two of its elements may not share a place (strides with which neighbours along one or
+ *    two axes do are refused).  Alignment: that of the element type.
  *  - Sums, statistics and states are fp32 whatever the type of the tensors, and what is stored is rounded once, to
  *    nearest.  Attention on RNN_BF16 tensors multiplies with the matrix instructions for bf16: the scores between frames of
  *    a chunk and, for outputs and gradients, the state that the chunk starts from go there in two bf16 numbers each, which
@@ -65,7 +66,8 @@ int rnn_linear_attention_forward(const rnn_linear_attention_desc* desc, const rn
                                  void* d_workspace, int64_t ws_bytes, void* hip_stream);
 
 /* Gradients from d_o = dE/do and d_dstate_out = dE/d state_out (float, or NULL: zero).  dq, dk, dv and
- * d_dstate_in (dE/d state_in, float) are overwritten; any of them may be NULL.  dk and dv are sums over
+ * d_dstate_in (dE/d state_in, float) are overwritten; any of them may be NULL.  d_dstate_in may be neither
+ * d_dstate_out nor, if dq is asked for, d_state_in.  dk and dv are sums over
  * the heads that share a key / value head, in a fixed order: same bits from call to call.  Frames behind
  * a stream's length stay as they were. */
 int rnn_linear_attention_backward(const rnn_linear_attention_desc* desc, const rnn_frames* q, const rnn_frames* k,

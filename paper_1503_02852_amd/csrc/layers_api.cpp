@@ -130,6 +130,19 @@ int check_places(const char* name, const rnn_frames* f, const rnn_linear_attenti
     }
     return shared && d->T > 0 ? invalid(std::string("attention: elements of ") + name + " share places") : RNN_OK;
 }
+// Outputs begin where nothing else of the call does.
+struct Start { const char* name; const void* p; };
+Start start(const char* name, const rnn_frames* f) { return Start{name, f ? f->data : nullptr}; }
+int check_apart(std::initializer_list<Start> outputs, std::initializer_list<Start> inputs) {
+    for (const Start& a : outputs) {
+        if (!a.p) continue;
+        for (const Start& b : outputs)
+            if (&a != &b && a.p == b.p) return invalid(std::string("attention: ") + a.name + " and " + b.name + " are one place");
+        for (const Start& b : inputs)
+            if (a.p == b.p) return invalid(std::string("attention: ") + a.name + " may not be " + b.name);
+    }
+    return RNN_OK;
+}
 int check_floats(const char* name, const void* p) { return misaligned(p, 4) ? invalid(std::string("attention: ") + name + " is not aligned to its type") : RNN_OK; }
 
 AttnTensor tensor(const rnn_frames* f, int group) { return f ? AttnTensor{f->data, f->stride_t, f->stride_n, f->stride_h, group} : AttnTensor{nullptr, 0, 0, 0, group}; }
@@ -222,6 +235,7 @@ int rnn_linear_attention_forward(const rnn_linear_attention_desc* d, const rnn_f
         if (!rc) rc = check_workspace(d_workspace, ws_bytes, w.total);
         if (rc || d->N == 0) return rc;
         if ((rc = check_places("o", o, d, d->heads, d->dim_v))) return rc;
+        if (d->T > 0 && (rc = check_apart({start("o", o)}, {start("q", q), start("k", k), start("v", v)}))) return rc;
         AttnOp a = forward_op(d, q, k, v);
         if (with_o) a.o = output(o);
         a.s_in = d_state_in; a.s_out = d_state_out;
@@ -256,6 +270,8 @@ int rnn_linear_attention_backward(const rnn_linear_attention_desc* d, const rnn_
         if ((rc = check_places("dq", dq, d, d->heads, d->dim_k))) return rc;
         if ((rc = check_places("dk", dk, d, d->kv_heads, d->dim_k))) return rc;
         if ((rc = check_places("dv", dv, d, d->kv_heads, d->dim_v))) return rc;
+        if (d->T > 0 && (rc = check_apart({start("dq", dq), start("dk", dk), start("dv", dv)}, {start("q", q), start("k", k), start("v", v), start("do", d_o)}))) return rc;
+        if (with_q && d_dstate_in && d_dstate_in == d_state_in) return invalid("attention: dstate_in may not be state_in, which dq is made from");
         hipStream_t s = static_cast<hipStream_t>(hip_stream);
         const int group = d->heads / d->kv_heads;
         const AttnCall call = call_of(d, d_log_decay, d_lengths);

@@ -181,3 +181,23 @@ def test_outputs_in_the_place_of_inputs():
     refused(b(norm(), P, 40, None, 0, Q, 48, P, None, Q, 40, None, 0, None, None, 0, None), "dx may not be h with another ld")
     refused(b(norm(), P, 40, None, 0, Q, 40, P, None, R, 40, R, 40, None, None, 0, None), "dx and dresidual are one place")
     refused(lib.rnn_dropout(drop(), P, 48, P, 40, None), "y may not be x with another ld")
+
+
+def test_attention_outputs_in_the_place_of_inputs_are_refused():
+    """Other workgroups still read them."""
+    lib = load_library()
+    d = attention(kv_heads=4, dim_k=24)
+    at = lambda i: C.byref(Frames(i * P, 192, 96, 24))  # noqa: E731
+    fwd = lambda o: lib.rnn_linear_attention_forward(d, at(1), at(2), at(3), P, None, None, None, o, P, 1 << 30, None)  # noqa: E731
+    for i, name in enumerate(("q", "k", "v")):
+        refused(fwd(at(i + 1)), f"o may not be {name}")
+
+    def back(dq, dk, dv, state=None, dstate=None):
+        return lib.rnn_linear_attention_backward(d, at(1), at(2), at(3), P, None, state, at(4), None, dq, dk, dv, dstate, P, 1 << 30, None)
+    for i, name in enumerate(("q", "k", "v", "do")):
+        refused(back(at(i + 1), None, None), f"dq may not be {name}")
+        refused(back(at(8), at(i + 1), None), f"dk may not be {name}")
+        refused(back(at(8), None, at(i + 1)), f"dv may not be {name}")
+    refused(back(at(8), at(8), at(9)), "dq and dk are one place")
+    refused(back(at(9), at(8), at(8)), "dk and dv are one place")
+    refused(back(at(9), None, None, 10 * P, 10 * P), "dstate_in may not be state_in")
