@@ -162,7 +162,9 @@ int rnn_forward(rnn_graph* g, const float* d_weights, const float* const* d_inpu
  * window computed in pieces equals the window computed at once (to the last bit, but where products of
  * 1,024 columns and more over few rows are shared by several workgroups, whose parts are added in any
  * order; rnn_set_deterministic keeps to one; and but for attention nodes, whose sums are grouped by chunks
- * counted from the piece's first frame: equal within fp32 rounding).  Arguments as in rnn_forward,
+ * counted from the piece's first frame: equal within fp32 rounding; once a call on the handle has been captured
+ * into a HIP graph, a piece goes over the keys and values of the window's earlier frames again, unless the capture
+ * that it is in has computed or shifted to the frames before it).  Arguments as in rnn_forward,
  * which is rnn_forward_range(.., 0, T, ..).  A call with t_begin = 0 starts a fresh window: zero
  * state in front of it, control words cleared.  rnn_bptt needs the whole window computed. */
 int rnn_forward_range(rnn_graph* g, const float* d_weights, const float* const* d_inputs,
